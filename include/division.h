@@ -68,7 +68,7 @@ typedef enum div_status {
     DIV_ERR_TIMEOUT = 7    /* device side: a bounded wait inside the fused kernel ran out  */
 } div_status;
 
-typedef enum div_dtype { DIV_F32 = 0, DIV_BF16 = 1 } div_dtype;
+typedef enum div_dtype { DIV_F32 = 0, DIV_BF16 = 1, DIV_F16 = 2 /* the operators of language models alone */ } div_dtype;
 
 /* Problem statement: tensor shape, block size B, bit width Q, dtypes (Sec. 4.1). */
 typedef struct div_desc {
@@ -342,6 +342,95 @@ div_status div_dropout_forward(const void* x_dev, void* y_dev, void* mask_dev, s
                                int32_t dtype, uint64_t seed, uint32_t drop_threshold, void* cuda_stream);
 div_status div_mask_backward(const void* mask_dev, size_t mask_bytes, const void* grad_out_dev, void* grad_in_dev,
                              uint64_t total, int32_t dtype, void* cuda_stream);
+
+/*
+ * ---- Operators of language models -------------------------------------------------------------------------------------
+ *
+ * Linear layers whose operands are held in 8 or 4 bits, the normalisation that feeds them and the log probabilities at the
+ * end.  (The paper has no counterpart; its subject, activations cached in few bits, is what the operands by columns are for.)
+ * Matrices are row-major with neighbours along a row; `row_stride` counts elements between the beginnings of two rows.
+ * rows, cols: 1 .. 2^31 - 513.  Dtypes: DIV_F32, DIV_BF16, DIV_F16.  Element pointers need the alignment of their type, blobs
+ * and workspaces 16 bytes; rows that begin at multiples of 16 bytes are read faster.  Infinities and NaNs are allowed.
+ * Outputs may not alias inputs.  All calls enqueue their work on the stream and return; results do not depend on timing.
+ */
+
+/*
+ * Microscaled matrices.  The rows of a matrix are cut into blocks of 32 neighbours (the last one of a row may be shorter).  A
+ * block holds one scale, a power of two in 8 bits, and a code for each number:
+ *   DIV_MX_E4M3  8-bit codes (4 bits of exponent, 3 of fraction; largest number 448)
+ *   DIV_MX_E2M1  4-bit codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives)
+ * scale = the smallest power of two with which the block's largest magnitude does not pass the largest number of the format,
+ * between 2^-127 and 2^127; code = value / scale, rounded to nearest, ties to even.  A block that holds an infinity or a NaN reads
+ * back as NaN.  A blob (codes | scales) is laid out for div_mx_matmul; div_mx_dequantize reads it back.  What a blob holds
+ * behind the last row is unspecified.
+ */
+typedef enum div_mx_format { DIV_MX_E4M3 = 0, DIV_MX_E2M1 = 1 } div_mx_format;
+typedef struct div_mx_layout {
+    uint64_t codes_off, codes_bytes;
+    uint64_t scales_off, scales_bytes;
+    uint64_t total_bytes;        /* blob size to allocate: whole tiles                                     */
+    uint64_t closed_form_bytes;  /* one byte and 32 codes for each block                                    */
+} div_mx_layout;
+div_status div_mx_bytes(int64_t rows, int64_t cols, int32_t format, div_mx_layout* out);
+/*
+ * Quantise x.  by_rows_dev receives the blob of x (rows x cols), by_columns_dev that of its transpose (cols x rows: blocks of
+ * 32 neighbours down a column of x, what a product that sums over the rows of x takes); either may be NULL.  Both come from one
+ * reading of x.
+ */
+div_status div_mx_quantize(const void* x_dev, int64_t rows, int64_t cols, int64_t row_stride, int32_t x_dtype, int32_t format,
+                           void* by_rows_dev, size_t by_rows_capacity, void* by_columns_dev, size_t by_columns_capacity, void* cuda_stream);
+/* out (rows x cols, contiguous) = the numbers a blob stands for, rounded to out_dtype (exact in float32 and bfloat16 between
+   2^-126 and their largest number, past which rounding up may lead). */
+div_status div_mx_dequantize(const void* blob_dev, size_t blob_bytes, int64_t rows, int64_t cols, int32_t format, void* out_dev,
+                             int32_t out_dtype, void* cuda_stream);
+
+/*
+ * out (m x n) = A * B^T from two blobs by rows with the same format: A is m x k, B is n x k.  Products and sums in 32 bits,
+ * rounded to out_dtype once.  (Should a bounded wait inside the kernel run out, its part of out is NaN.)
+ */
+div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
+                         void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream);
+
+/*
+ * Root-mean-square normalisation with the residual's addition.
+ *   h = x + residual, rounded to dtype (residual_dev NULL: h = x, and h_dev is NULL too)
+ *   y = h * rstd * weight,  rstd = 1 / sqrt(mean over the row of h^2 + eps)
+ * y_dev receives y in dtype, blob_dev y quantised by rows (div_mx_quantize's blob of y before it is rounded to dtype); at least one of
+ * the two.  rstd_dev (float32, one a row; NULL: not kept) is what the backward pass wants.  h, y: rows x cols, contiguous.
+ * weight_dtype: dtype or DIV_F32.  Sums in 32 bits.
+ */
+div_status div_rms_norm_forward(const void* x_dev, int64_t x_row_stride, const void* residual_dev, int64_t residual_row_stride,
+                                const void* weight_dev, int32_t weight_dtype, int64_t rows, int64_t cols, int32_t dtype, float eps, void* h_dev,
+                                void* y_dev, void* blob_dev, size_t blob_capacity, int32_t format, float* rstd_dev, void* cuda_stream);
+/*
+ * dx = dh + rstd * (weight dy - n * mean(weight dy n)), n = h * rstd: the gradient of x and, the same, of the residual (dh_dev NULL: 0).
+ * dweight = sum over rows of dy n, in weight_dtype (NULL: not wanted; else a workspace of div_rms_norm_workspace bytes, whose contents
+ * on entry do not matter; two calls that overlap on the GPU must not share one).  dx: contiguous.
+ */
+div_status div_rms_norm_workspace(int64_t rows, int64_t cols, uint64_t* out_bytes);
+div_status div_rms_norm_backward(const void* dy_dev, int64_t dy_row_stride, const void* dh_dev, int64_t dh_row_stride, const void* h_dev,
+                                 int64_t h_row_stride, const void* weight_dev, int32_t weight_dtype, const float* rstd_dev, int64_t rows, int64_t cols,
+                                 int32_t dtype, void* dx_dev, void* dweight_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Log probabilities of given tokens under softmax(logits), with the distribution's entropy and its most probable tokens.
+ *   logprobs[i] = logits[i, targets[i]] - log sum exp(logits[i]);  a negative target is none: 0;  one behind the vocabulary: NaN
+ *   entropy[i]  = - sum over j of p log p
+ *   top_logprobs, top_indices (rows x top, 0 <= top <= 32, top <= vocab): the largest, equal ones by index, a NaN above all
+ *   stats[i]    = what the backward pass wants: the row's largest logit m, and log sum exp(logits - m)
+ * Logits of -inf have probability 0.  A row of nothing else has no distribution: log probabilities -inf, entropy 0, gradient 0.  A row that
+ * holds NaN or +inf gives NaN.  All results are float32, indices and targets int64.  vocab < 2^31 - 512.
+ */
+div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride, int64_t rows, int64_t vocab, int32_t dtype, const int64_t* targets_dev,
+                                      int32_t top, float* logprobs_dev, float* entropy_dev, float* stats_dev, float* top_logprobs_dev,
+                                      int64_t* top_indices_dev, void* cuda_stream);
+/*
+ * dlogits[i, j] = dlogprobs[i] * ([j = targets[i]] - p) - dentropy[i] * p * (log p + entropy[i]), rounded to dtype; contiguous.
+ * dlogprobs_dev or dentropy_dev may be NULL (0).
+ */
+div_status div_token_logprobs_backward(const void* logits_dev, int64_t row_stride, int64_t rows, int64_t vocab, int32_t dtype, const int64_t* targets_dev,
+                                       const float* stats_dev, const float* entropy_dev, const float* dlogprobs_dev, const float* dentropy_dev,
+                                       void* dlogits_dev, void* cuda_stream);
 
 /* Which kernels a descriptor maps to on the current device.  desc, out: host. */
 div_status div_plan_query(const div_desc* desc, uint32_t flags, div_plan* out);

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
+from ctypes import c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdivision.so")
 
@@ -25,6 +25,9 @@ DIV_FLAG_NO_STAGED_KERNEL = 32
 DIV_FLAG_TWO_LAUNCH_PLANES = 64
 DIV_FLAG_NO_PARK_KERNEL = 256
 DTYPE_CODES = {"f32": DIV_F32, "bf16": DIV_BF16}
+DIV_F16 = 2                                         # the operators of language models alone
+LM_DTYPE_CODES = {"f32": DIV_F32, "bf16": DIV_BF16, "f16": DIV_F16}
+MX_FORMATS = {"e4m3": 0, "e2m1": 1}
 
 EXPORTED_SYMBOLS = (
     "div_compressed_bytes", "div_compress", "div_compress_ex", "div_compress_static", "div_read_static_status",
@@ -34,6 +37,9 @@ EXPORTED_SYMBOLS = (
     "div_mask_bytes", "div_relu_forward", "div_dropout_forward", "div_mask_backward",
     "div_planegroup_bytes", "div_planegroup_compress", "div_planegroup_decompress", "div_planegroup_plan_query",
     "div_read_device_status", "div_status_string",
+    "div_mx_bytes", "div_mx_quantize", "div_mx_dequantize", "div_mx_matmul",
+    "div_rms_norm_forward", "div_rms_norm_workspace", "div_rms_norm_backward",
+    "div_token_logprobs_forward", "div_token_logprobs_backward",
 )
 
 
@@ -57,6 +63,10 @@ class DivPlan(ctypes.Structure):
     _fields_ = [("fused", c_int32), ("grid", c_int32), ("threads", c_int32), ("stages", c_int32),
                 ("lag", c_int32), ("smem_bytes", c_int32), ("chunk_elems", c_int64),
                 ("chunks_per_sample", c_int64), ("decompress_fast", c_int32), ("on_chip", c_int32), ("parked", c_int32)]
+
+
+class DivMxLayout(ctypes.Structure):
+    _fields_ = [(name, c_uint64) for name in ("codes_off", "codes_bytes", "scales_off", "scales_bytes", "total_bytes", "closed_form_bytes")]
 
 
 class DivisionError(RuntimeError):
@@ -124,6 +134,28 @@ def lib() -> ctypes.CDLL:
         L.div_mask_backward.restype = c_int32
         L.div_read_device_status.argtypes = [c_void_p, c_void_p, ctypes.POINTER(c_int32)]
         L.div_read_device_status.restype = c_int32
+        L.div_mx_bytes.argtypes = [c_int64, c_int64, c_int32, ctypes.POINTER(DivMxLayout)]
+        L.div_mx_bytes.restype = c_int32
+        L.div_mx_quantize.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int32, c_int32, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p]
+        L.div_mx_quantize.restype = c_int32
+        L.div_mx_dequantize.argtypes = [c_void_p, c_size_t, c_int64, c_int64, c_int32, c_void_p, c_int32, c_void_p]
+        L.div_mx_dequantize.restype = c_int32
+        L.div_mx_matmul.argtypes = [c_void_p, c_size_t, c_void_p, c_size_t, c_int64, c_int64, c_int64, c_int32, c_void_p, c_int64, c_int32, c_void_p]
+        L.div_mx_matmul.restype = c_int32
+        L.div_rms_norm_forward.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_int64, c_int64, c_int32, c_float, c_void_p,
+                                           c_void_p, c_void_p, c_size_t, c_int32, c_void_p, c_void_p]
+        L.div_rms_norm_forward.restype = c_int32
+        L.div_rms_norm_workspace.argtypes = [c_int64, c_int64, ctypes.POINTER(c_uint64)]
+        L.div_rms_norm_workspace.restype = c_int32
+        L.div_rms_norm_backward.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int64, c_int64,
+                                            c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.div_rms_norm_backward.restype = c_int32
+        L.div_token_logprobs_forward.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                                 c_void_p, c_void_p, c_void_p]
+        L.div_token_logprobs_forward.restype = c_int32
+        L.div_token_logprobs_backward.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                                  c_void_p, c_void_p]
+        L.div_token_logprobs_backward.restype = c_int32
         L.div_status_string.argtypes = [c_int32]
         L.div_status_string.restype = c_char_p
         _lib = L
@@ -265,6 +297,64 @@ def div_mask_backward(mask_ptr: int, mask_bytes: int, grad_out_ptr: int, grad_in
                       dtype: str = "f32", stream: int = 0) -> None:
     _check(lib().div_mask_backward(c_void_p(mask_ptr), mask_bytes, c_void_p(grad_out_ptr), c_void_p(grad_in_ptr),
                                    c_uint64(total), DTYPE_CODES[dtype], c_void_p(stream)), "div_mask_backward")
+
+
+# The operators of language models (raw pointers; paper_2208_04187_b200.language has them on torch tensors).
+def div_mx_bytes(rows: int, cols: int, fmt: str = "e4m3") -> DivMxLayout:
+    out = DivMxLayout()
+    _check(lib().div_mx_bytes(rows, cols, MX_FORMATS[fmt], ctypes.byref(out)), "div_mx_bytes")
+    return out
+
+
+def div_mx_quantize(x_ptr: int, rows: int, cols: int, row_stride: int, dtype: str, fmt: str, rows_ptr: int | None, rows_capacity: int,
+                    columns_ptr: int | None, columns_capacity: int, stream: int = 0) -> None:
+    _check(lib().div_mx_quantize(x_ptr, rows, cols, row_stride, LM_DTYPE_CODES[dtype], MX_FORMATS[fmt], rows_ptr, rows_capacity, columns_ptr,
+                                 columns_capacity, stream), "div_mx_quantize")
+
+
+def div_mx_dequantize(blob_ptr: int, blob_bytes: int, rows: int, cols: int, fmt: str, out_ptr: int, dtype: str, stream: int = 0) -> None:
+    _check(lib().div_mx_dequantize(blob_ptr, blob_bytes, rows, cols, MX_FORMATS[fmt], out_ptr, LM_DTYPE_CODES[dtype], stream), "div_mx_dequantize")
+
+
+def div_mx_matmul(a_ptr: int, a_bytes: int, b_ptr: int, b_bytes: int, m: int, n: int, k: int, fmt: str, out_ptr: int, out_row_stride: int,
+                  dtype: str, stream: int = 0) -> None:
+    _check(lib().div_mx_matmul(a_ptr, a_bytes, b_ptr, b_bytes, m, n, k, MX_FORMATS[fmt], out_ptr, out_row_stride, LM_DTYPE_CODES[dtype], stream),
+           "div_mx_matmul")
+
+
+def div_rms_norm_forward(x_ptr: int, x_row_stride: int, residual_ptr: int | None, residual_row_stride: int, weight_ptr: int, weight_dtype: str,
+                         rows: int, cols: int, dtype: str, eps: float, h_ptr: int | None, y_ptr: int | None, blob_ptr: int | None,
+                         blob_capacity: int, fmt: str, rstd_ptr: int | None, stream: int = 0) -> None:
+    _check(lib().div_rms_norm_forward(x_ptr, x_row_stride, residual_ptr, residual_row_stride, weight_ptr, LM_DTYPE_CODES[weight_dtype], rows, cols,
+                                      LM_DTYPE_CODES[dtype], eps, h_ptr, y_ptr, blob_ptr, blob_capacity, MX_FORMATS[fmt], rstd_ptr, stream),
+           "div_rms_norm_forward")
+
+
+def div_rms_norm_workspace(rows: int, cols: int) -> int:
+    out = c_uint64(0)
+    _check(lib().div_rms_norm_workspace(rows, cols, ctypes.byref(out)), "div_rms_norm_workspace")
+    return out.value
+
+
+def div_rms_norm_backward(dy_ptr: int, dy_row_stride: int, dh_ptr: int | None, dh_row_stride: int, h_ptr: int, h_row_stride: int, weight_ptr: int,
+                          weight_dtype: str, rstd_ptr: int, rows: int, cols: int, dtype: str, dx_ptr: int, dweight_ptr: int | None,
+                          ws_ptr: int | None, ws_bytes: int, stream: int = 0) -> None:
+    _check(lib().div_rms_norm_backward(dy_ptr, dy_row_stride, dh_ptr, dh_row_stride, h_ptr, h_row_stride, weight_ptr, LM_DTYPE_CODES[weight_dtype],
+                                       rstd_ptr, rows, cols, LM_DTYPE_CODES[dtype], dx_ptr, dweight_ptr, ws_ptr, ws_bytes, stream),
+           "div_rms_norm_backward")
+
+
+def div_token_logprobs_forward(logits_ptr: int, row_stride: int, rows: int, vocab: int, dtype: str, targets_ptr: int, top: int, logprobs_ptr: int,
+                               entropy_ptr: int, stats_ptr: int, top_logprobs_ptr: int | None, top_indices_ptr: int | None, stream: int = 0) -> None:
+    _check(lib().div_token_logprobs_forward(logits_ptr, row_stride, rows, vocab, LM_DTYPE_CODES[dtype], targets_ptr, top, logprobs_ptr, entropy_ptr,
+                                            stats_ptr, top_logprobs_ptr, top_indices_ptr, stream), "div_token_logprobs_forward")
+
+
+def div_token_logprobs_backward(logits_ptr: int, row_stride: int, rows: int, vocab: int, dtype: str, targets_ptr: int, stats_ptr: int,
+                                entropy_ptr: int | None, dlogprobs_ptr: int | None, dentropy_ptr: int | None, dlogits_ptr: int,
+                                stream: int = 0) -> None:
+    _check(lib().div_token_logprobs_backward(logits_ptr, row_stride, rows, vocab, LM_DTYPE_CODES[dtype], targets_ptr, stats_ptr, entropy_ptr,
+                                             dlogprobs_ptr, dentropy_ptr, dlogits_ptr, stream), "div_token_logprobs_backward")
 
 
 def div_read_device_status(ws_ptr: int, stream: int = 0) -> int:

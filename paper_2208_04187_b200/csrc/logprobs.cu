@@ -1,0 +1,485 @@
+// Log probabilities of given tokens, entropies, the most probable tokens, and the gradient of the logits.
+//
+//   m = max x,  s = sum exp(x - m),  t = sum (x - m) exp(x - m)          (one pass: running values, rescaled when m grows)
+//   log p_j = (x_j - m) - log s,     entropy = log s - t / s
+//   dx_j = dlp ([j = target] - p_j) - dH p_j (log p_j + H)
+// m and log s are kept apart: their sum would lose log s next to a large m.
+//
+// Forward is bound by memory where the vocabulary is long (one reading of the logits), by the exponentials next (16 a clock and SM).  A
+// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, and joins its sums with the others' in a
+// fixed order.
+//
+// The most probable tokens come from the same pass: the k-th largest of the CTA's threads' maxima is a bound that at least k logits
+// reach, so that only threads whose maximum reaches it (about k of them) have their pieces read again, out of L2, by whole warps.  What passes
+// the bound goes into a sorted list across a warp's lanes; the warps' lists, and the cluster's, are joined by counting ranks.
+#include "mx.cuh"
+
+namespace divk {
+
+constexpr uint32_t LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_MAX_TOP = 32, LP_MAX_CLUSTER = 8;
+constexpr float LP_LOG2E = 1.4426950408889634f;
+constexpr float LP_LEAST = -1000.f;             // exp of it is 0, and 0 times it is no NaN
+
+struct LogprobParams {
+    const void* x;
+    uint64_t stride;
+    uint32_t rows, vocab;
+    const int64_t* targets;
+    uint32_t top, split;
+    float *logprobs, *entropy, *stats, *top_logprobs;
+    int64_t* top_indices;
+};
+
+struct Running {
+    float m, s, t;
+};
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float v;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ float exp2_fast(float a) {
+    float v;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(v) : "f"(a));
+    return v;
+}
+// brings r to a larger maximum
+__device__ __forceinline__ void rescale(Running& r, float m) {
+    if (m > r.m) {
+        if (r.m != -INFINITY) {                        // (else nothing has been summed)
+            const float d = max_nan(r.m - m, LP_LEAST), c = exp2_fast(d * LP_LOG2E);
+            r.t = c * fmaf(r.s, d, r.t);
+            r.s = c * r.s;
+        }
+        r.m = m;
+    }
+}
+__device__ __forceinline__ Running join(Running a, const Running& b) {
+    Running c = b;
+    rescale(a, c.m);
+    rescale(c, a.m);
+    a.s += c.s;
+    a.t += c.t;
+    return a;
+}
+// a number of the row: r.m is at least x
+__device__ __forceinline__ void take(Running& r, float base, float x) {
+    const float a = max_nan(x - base, LP_LEAST), e = exp2_fast(a * LP_LOG2E);
+    r.s += e;
+    r.t = fmaf(e, a, r.t);
+}
+template <int N>
+__device__ __forceinline__ void take_all(Running& r, const float (&v)[N]) {
+    float m = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+    rescale(r, m);
+    const float base = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) take(r, base, v[i]);
+}
+
+// ---------------------------------------------------------------------------------------------
+// 16-byte pieces of a row that may begin anywhere: piece 0 ends at the first multiple of 16 bytes
+// ---------------------------------------------------------------------------------------------
+template <typename T> struct Pieces {
+    static constexpr uint32_t N = 16u / sizeof(T);
+    const T* row;
+    uint32_t first, count, vocab;                // numbers before the first whole piece (0..N-1); pieces in all
+    __device__ __forceinline__ Pieces(const T* r, uint32_t v) : row(r), vocab(v) {
+        first = (uint32_t)((16u - (reinterpret_cast<uintptr_t>(r) & 15u)) & 15u) / (uint32_t)sizeof(T);
+        if (first > v) first = v;
+        count = (first ? 1u : 0u) + (v - first + N - 1u) / N;
+    }
+    // index of the first number of a piece, and how many it has
+    __device__ __forceinline__ uint32_t begin(uint32_t piece) const { return first ? (piece ? first + (piece - 1u) * N : 0u) : piece * N; }
+    __device__ __forceinline__ uint32_t size(uint32_t piece) const {
+        const uint32_t b = begin(piece), full = first && piece == 0 ? first : N;
+        return min(full, vocab - b);
+    }
+    // numbers that are not there are -inf
+    __device__ __forceinline__ void get(uint32_t piece, float (&v)[N]) const {
+        const T* p = row + begin(piece);
+        const uint32_t n = size(piece);
+        if (n == N) {
+            unpack(*reinterpret_cast<const uint4*>(p), v);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) v[i] = i < n ? to_f32(p[i]) : -INFINITY;
+        }
+    }
+    static __device__ __forceinline__ void unpack(const uint4& q, float (&v)[N]) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) {
+                const unsigned short h = (unsigned short)(w[i >> 1] >> (16u * (i & 1u)));
+                v[i] = to_f32(*reinterpret_cast<const T*>(&h));
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------------------
+// the most probable tokens: (key, index) pairs, larger keys first, then smaller indices
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t order_key(float x) { return x != x ? 0xFFFFFFFFu : float_key(x + 0.f); }     // (-0 is 0; key 0 is nobody's)
+__device__ __forceinline__ float key_value(uint32_t k) { return k == 0xFFFFFFFFu ? __uint_as_float(0x7FC00000u) : key_float(k); }
+__device__ __forceinline__ bool before(uint32_t ka, uint32_t ia, uint32_t kb, uint32_t ib) { return ka > kb || (ka == kb && ia < ib); }
+
+struct TopList {            // across the lanes of a warp, best first
+    uint32_t key, index;
+    __device__ __forceinline__ void offer(bool have, uint32_t k, uint32_t i, uint32_t top, uint32_t& last_key, uint32_t& last_index) {
+        const uint32_t lane = threadIdx.x & 31u;
+        uint32_t who = __ballot_sync(0xFFFFFFFFu, have && before(k, i, last_key, last_index));
+        while (who) {
+            const uint32_t src = (uint32_t)__ffs((int)who) - 1u;
+            who &= who - 1u;
+            const uint32_t ck = __shfl_sync(0xFFFFFFFFu, k, src), ci = __shfl_sync(0xFFFFFFFFu, i, src);
+            if (!before(ck, ci, last_key, last_index)) continue;
+            const uint32_t at = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, before(key, index, ck, ci)));
+            const uint32_t pk = __shfl_up_sync(0xFFFFFFFFu, key, 1), pi = __shfl_up_sync(0xFFFFFFFFu, index, 1);
+            if (lane == at) {
+                key = ck;
+                index = ci;
+            } else if (lane > at) {
+                key = pk;
+                index = pi;
+            }
+            last_key = __shfl_sync(0xFFFFFFFFu, key, top - 1u);
+            last_index = __shfl_sync(0xFFFFFFFFu, index, top - 1u);
+        }
+    }
+};
+
+struct LogprobShared {
+    Running warps[LP_WARPS];
+    Running cta;
+    alignas(16) uint32_t maxima[LP_THREADS];        // keys of the threads' maxima
+    uint32_t bound, n_again;
+    uint32_t again[LP_THREADS];                     // threads whose pieces are read again
+    uint32_t key[LP_THREADS], index[LP_THREADS];     // the warps' lists, then (of rank 0) the cluster's
+    uint32_t best_key[LP_MAX_TOP], best_index[LP_MAX_TOP];
+};
+static_assert(LP_WARPS * LP_MAX_TOP == LP_THREADS && LP_MAX_CLUSTER * LP_MAX_TOP <= LP_THREADS, "a list entry for each thread");
+
+__device__ __forceinline__ uint32_t lp_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t lp_peer(uint32_t local, uint32_t rank) {
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+// the `top` best of the entries in sh.key, sh.index go to sh.best_key, sh.best_index (key 0: no entry); all threads together
+__device__ __forceinline__ void lp_rank_entries(LogprobShared& sh, uint32_t top) {
+    const uint32_t k = sh.key[threadIdx.x], i = sh.index[threadIdx.x];
+    if (k != 0u) {
+        uint32_t better = 0;
+        for (uint32_t j = 0; j < LP_THREADS; ++j) better += before(sh.key[j], sh.index[j], k, i) ? 1u : 0u;
+        if (better < top) {
+            sh.best_key[better] = k;
+            sh.best_index[better] = i;
+        }
+    }
+}
+
+template <typename XT, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS)
+logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
+    typedef Pieces<XT> P;
+    __shared__ LogprobShared sh;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t row = blockIdx.x / p.split, rank = p.split > 1u ? lp_rank() : 0u;
+    griddep_wait();
+    griddep_launch();
+    const P pieces(static_cast<const XT*>(p.x) + row * p.stride, p.vocab);
+    const uint32_t from = (uint32_t)((uint64_t)pieces.count * rank / p.split), to = (uint32_t)((uint64_t)pieces.count * (rank + 1u) / p.split);
+
+    Running r = {-INFINITY, 0.f, 0.f};
+    constexpr uint32_t AT_ONCE = 4;
+    uint32_t piece = from + threadIdx.x;
+    for (; piece + (AT_ONCE - 1u) * LP_THREADS < to; piece += AT_ONCE * LP_THREADS) {
+        float v[AT_ONCE][P::N];
+#pragma unroll
+        for (uint32_t u = 0; u < AT_ONCE; ++u) pieces.get(piece + u * LP_THREADS, v[u]);
+#pragma unroll
+        for (uint32_t u = 0; u < AT_ONCE; ++u) take_all(r, v[u]);
+    }
+    for (; piece < to; piece += LP_THREADS) {
+        float v[P::N];
+        pieces.get(piece, v);
+        take_all(r, v);
+    }
+    const float thread_max = r.m;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        Running o;
+        o.m = __shfl_xor_sync(0xFFFFFFFFu, r.m, d);
+        o.s = __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
+        o.t = __shfl_xor_sync(0xFFFFFFFFu, r.t, d);
+        // (both lanes of a pair join in the same order, so that they agree to the bit)
+        const bool low = (lane & d) == 0;
+        r = join(low ? r : o, low ? o : r);
+    }
+    if (lane == 0) sh.warps[warp] = r;
+    if (TOP) {
+        sh.maxima[threadIdx.x] = from + threadIdx.x < to ? order_key(thread_max) : 0u;
+        if (threadIdx.x == 0) sh.n_again = 0;
+    }
+    __syncthreads();
+    r = sh.warps[0];
+    for (uint32_t w = 1; w < LP_WARPS; ++w) r = join(r, sh.warps[w]);
+    if (threadIdx.x == 0) sh.cta = r;
+
+    if (TOP) {
+        // the top-th largest of the threads' maxima; 0 (everything) where not that many threads had a piece.  A sum that is NaN may come
+        // from a NaN, which no maximum shows: everything is read again.
+        const uint32_t mine = sh.maxima[threadIdx.x];
+        uint32_t above = 0, reach = 0;
+        for (uint32_t j = 0; j < LP_THREADS; j += 4) {
+            const uint4 k = *reinterpret_cast<const uint4*>(&sh.maxima[j]);
+            above += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
+            reach += (k.x >= mine) + (k.y >= mine) + (k.z >= mine) + (k.w >= mine);
+        }
+        if (above < p.top && reach >= p.top) sh.bound = mine;       // (all that write, write the same)
+        __syncthreads();
+        const uint32_t bound = r.s != r.s ? 0u : sh.bound;
+        if (from + threadIdx.x < to && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1u)] = threadIdx.x;
+        __syncthreads();
+        TopList list = {0u, 0xFFFFFFFFu};
+        uint32_t last_key = 0u, last_index = 0xFFFFFFFFu;
+        const uint32_t each = (to - from + LP_THREADS - 1u) / LP_THREADS;          // pieces of a thread, at most
+        const uint32_t runs = (each + 31u) / 32u, jobs = sh.n_again * runs;
+        for (uint32_t job = warp; job < jobs; job += LP_WARPS) {
+            const uint32_t at = from + sh.again[job / runs] + (job % runs * 32u + lane) * LP_THREADS;
+            float v[P::N];
+#pragma unroll
+            for (uint32_t i = 0; i < P::N; ++i) v[i] = -INFINITY;
+            const uint32_t n = at < to ? pieces.size(at) : 0u, first = at < to ? pieces.begin(at) : 0u;
+            if (n) pieces.get(at, v);
+#pragma unroll
+            for (uint32_t i = 0; i < P::N; ++i) {
+                const uint32_t k = order_key(v[i]);
+                list.offer(i < n && k >= bound, k, first + i, p.top, last_key, last_index);
+            }
+        }
+        sh.key[threadIdx.x] = lane < p.top ? list.key : 0u;
+        sh.index[threadIdx.x] = lane < p.top ? list.index : 0xFFFFFFFFu;
+        if (threadIdx.x < LP_MAX_TOP) {                    // (a CTA of a cluster may hold fewer than `top`)
+            sh.best_key[threadIdx.x] = 0u;
+            sh.best_index[threadIdx.x] = 0xFFFFFFFFu;
+        }
+        __syncthreads();
+        lp_rank_entries(sh, p.top);
+    }
+    if (p.split > 1u) {
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (rank == 0) {
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(&sh.cta);
+            for (uint32_t c = 1; c < p.split; ++c) {
+                Running o;
+                o.m = __uint_as_float(lp_peer(at, c));
+                o.s = __uint_as_float(lp_peer(at + 4u, c));
+                o.t = __uint_as_float(lp_peer(at + 8u, c));
+                r = join(r, o);
+            }
+            if (TOP) {
+                const uint32_t c = threadIdx.x / LP_MAX_TOP, e = threadIdx.x % LP_MAX_TOP;
+                uint32_t k = 0u, i = 0xFFFFFFFFu;
+                if (c < p.split) {
+                    k = lp_peer((uint32_t)__cvta_generic_to_shared(&sh.best_key[e]), c);
+                    i = lp_peer((uint32_t)__cvta_generic_to_shared(&sh.best_index[e]), c);
+                }
+                __syncthreads();
+                sh.key[threadIdx.x] = k;
+                sh.index[threadIdx.x] = i;
+                __syncthreads();
+                lp_rank_entries(sh, p.top);
+            }
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (rank != 0) return;
+    }
+    if (TOP) __syncthreads();
+    const bool empty = r.m == -INFINITY && r.s == 0.f;
+    const float m = empty ? 0.f : r.m, log_s = empty ? INFINITY : logf(r.s);
+    if (threadIdx.x == 0) {
+        const int64_t target = p.targets[row];
+        float lp = 0.f;
+        if (target >= (int64_t)p.vocab) lp = __uint_as_float(0x7FC00000u);
+        else if (target >= 0) lp = (to_f32(pieces.row[target]) - m) - log_s;
+        p.logprobs[row] = lp;
+        p.entropy[row] = empty ? 0.f : log_s - r.t / r.s;
+        p.stats[2ull * row] = m;
+        p.stats[2ull * row + 1u] = log_s;
+    }
+    if (TOP && threadIdx.x < p.top) {
+        p.top_logprobs[(uint64_t)row * p.top + threadIdx.x] = (key_value(sh.best_key[threadIdx.x]) - m) - log_s;
+        p.top_indices[(uint64_t)row * p.top + threadIdx.x] = (int64_t)sh.best_index[threadIdx.x];
+    }
+}
+
+struct LogprobBackParams {
+    const void* x;
+    uint64_t stride;
+    uint32_t rows, vocab;
+    const int64_t* targets;
+    const float *stats, *entropy, *dlogprobs, *dentropy;
+    void* dx;
+    uint32_t chunks;            // CTAs of a row
+};
+constexpr uint32_t LP_BACK_EACH = 4;          // pieces of a thread
+
+template <typename XT>
+__global__ void __launch_bounds__(LP_THREADS)
+logprob_backward_kernel(const __grid_constant__ LogprobBackParams p) {
+    typedef Pieces<XT> P;
+    griddep_wait();
+    griddep_launch();
+    const uint32_t row = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+    const P pieces(static_cast<const XT*>(p.x) + row * p.stride, p.vocab);
+    XT* out = static_cast<XT*>(p.dx) + (uint64_t)row * p.vocab;
+    const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(pieces.row)) & 15u) == 0;      // pieces begin alike
+    float v[LP_BACK_EACH][P::N];
+    const uint32_t first = chunk * LP_THREADS * LP_BACK_EACH + threadIdx.x;
+#pragma unroll
+    for (uint32_t u = 0; u < LP_BACK_EACH; ++u)
+        if (first + u * LP_THREADS < pieces.count) pieces.get(first + u * LP_THREADS, v[u]);
+    const float m = p.stats[2ull * row], log_s = p.stats[2ull * row + 1u];
+    const int64_t target = p.targets[row];
+    float dlp = p.dlogprobs ? p.dlogprobs[row] : 0.f;
+    if (target < 0 || log_s == INFINITY) dlp = 0.f;
+    else if (target >= (int64_t)p.vocab) dlp = __uint_as_float(0x7FC00000u);
+    const float dent = p.dentropy ? p.dentropy[row] : 0.f;
+    const float c0 = p.dentropy ? fmaf(dent, p.entropy[row], dlp) : dlp;
+    const uint32_t hit = target >= 0 && target < (int64_t)p.vocab ? (uint32_t)target : 0xFFFFFFFFu;
+#pragma unroll
+    for (uint32_t u = 0; u < LP_BACK_EACH; ++u) {
+        const uint32_t piece = first + u * LP_THREADS;
+        if (piece >= pieces.count) continue;
+        const uint32_t begin = pieces.begin(piece), n = pieces.size(piece);
+#pragma unroll
+        for (uint32_t i = 0; i < P::N; ++i) {
+            const float lp = max_nan((v[u][i] - m) - log_s, LP_LEAST), e = exp2_fast(lp * LP_LOG2E);
+            const float d = -e * fmaf(dent, lp, c0);
+            v[u][i] = begin + i == hit ? d + dlp : d;
+        }
+        if (n == P::N && same) {
+            uint32_t w[4];
+            if (sizeof(XT) == 4) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) w[i] = __float_as_uint(v[u][i]);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const XT a = from_f32<XT>(v[u][(2 * i) % P::N]), b = from_f32<XT>(v[u][(2 * i + 1) % P::N]);
+                    w[i] = *reinterpret_cast<const unsigned short*>(&a) | (uint32_t)*reinterpret_cast<const unsigned short*>(&b) << 16;
+                }
+            }
+            *reinterpret_cast<uint4*>(out + begin) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < P::N; ++i)
+                if (i < n) out[begin + i] = from_f32<XT>(v[u][i]);
+        }
+    }
+}
+
+}  // namespace divk
+
+namespace {
+using namespace divk;
+inline bool aligned_to(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+}  // namespace
+
+extern "C" {
+
+div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride, int64_t rows, int64_t vocab, int32_t dtype, const int64_t* targets_dev,
+                                      int32_t top, float* logprobs_dev, float* entropy_dev, float* stats_dev, float* top_logprobs_dev,
+                                      int64_t* top_indices_dev, void* cuda_stream) {
+    if (!logits_dev || !targets_dev || !logprobs_dev || !entropy_dev || !stats_dev || (top > 0 && (!top_logprobs_dev || !top_indices_dev))) return DIV_ERR_NULL;
+    if (!lm_size_ok(rows) || !lm_size_ok(vocab) || (rows > 1 && row_stride < vocab)) return DIV_ERR_SHAPE;
+    if (!lm_dtype_ok(dtype) || top < 0 || top > (int32_t)LP_MAX_TOP || top > vocab) return DIV_ERR_PARAM;
+    if (!aligned_to(logits_dev, lm_dtype_bytes(dtype)) || !aligned_to(targets_dev, 8) || !aligned_to(logprobs_dev, 4) || !aligned_to(entropy_dev, 4) ||
+        !aligned_to(stats_dev, 4) || !aligned_to(top_logprobs_dev, 4) || !aligned_to(top_indices_dev, 8))
+        return DIV_ERR_ALIGN;
+    LogprobParams p;
+    p.x = logits_dev;
+    p.stride = (uint64_t)row_stride;
+    p.rows = (uint32_t)rows;
+    p.vocab = (uint32_t)vocab;
+    p.targets = targets_dev;
+    p.top = (uint32_t)top;
+    p.logprobs = logprobs_dev;
+    p.entropy = entropy_dev;
+    p.stats = stats_dev;
+    p.top_logprobs = top_logprobs_dev;
+    p.top_indices = top_indices_dev;
+    // few rows: a cluster each, as long as every thread of it has a piece
+    const uint64_t pieces = (uint64_t)vocab * lm_dtype_bytes(dtype) / 16u;
+    uint32_t split = 1;
+    while (split < LP_MAX_CLUSTER && (uint64_t)rows * split < 296u && pieces >= 2ull * split * LP_THREADS) split *= 2u;
+    p.split = split;
+    if ((uint64_t)rows * split >= (1ull << 31)) return DIV_ERR_SHAPE;
+    return with_type(dtype, [&](auto* t) {
+        typedef std::remove_pointer_t<decltype(t)> XT;
+        auto kern = top ? logprob_forward_kernel<XT, true> : logprob_forward_kernel<XT, false>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((uint32_t)rows * split);
+        cfg.blockDim = dim3(LP_THREADS);
+        cfg.stream = (cudaStream_t)cuda_stream;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = split;
+        at[1].val.clusterDim.y = 1;
+        at[1].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+        if (cudaLaunchKernelEx(&cfg, kern, p) != cudaSuccess) {
+            cudaGetLastError();
+            return DIV_ERR_CUDA;
+        }
+        return DIV_OK;
+    });
+}
+
+div_status div_token_logprobs_backward(const void* logits_dev, int64_t row_stride, int64_t rows, int64_t vocab, int32_t dtype, const int64_t* targets_dev,
+                                       const float* stats_dev, const float* entropy_dev, const float* dlogprobs_dev, const float* dentropy_dev,
+                                       void* dlogits_dev, void* cuda_stream) {
+    if (!logits_dev || !targets_dev || !stats_dev || (dentropy_dev && !entropy_dev) || !dlogits_dev) return DIV_ERR_NULL;
+    if (!lm_size_ok(rows) || !lm_size_ok(vocab) || (rows > 1 && row_stride < vocab)) return DIV_ERR_SHAPE;
+    if (!lm_dtype_ok(dtype)) return DIV_ERR_PARAM;
+    if (!aligned_to(logits_dev, lm_dtype_bytes(dtype)) || !aligned_to(targets_dev, 8) || !aligned_to(stats_dev, 4) || !aligned_to(entropy_dev, 4) ||
+        !aligned_to(dlogprobs_dev, 4) || !aligned_to(dentropy_dev, 4) || !aligned_to(dlogits_dev, lm_dtype_bytes(dtype)))
+        return DIV_ERR_ALIGN;
+    LogprobBackParams p;
+    p.x = logits_dev;
+    p.stride = (uint64_t)row_stride;
+    p.rows = (uint32_t)rows;
+    p.vocab = (uint32_t)vocab;
+    p.targets = targets_dev;
+    p.stats = stats_dev;
+    p.entropy = entropy_dev;
+    p.dlogprobs = dlogprobs_dev;
+    p.dentropy = dentropy_dev;
+    p.dx = dlogits_dev;
+    const uint64_t each = 16u / lm_dtype_bytes(dtype), most = ((uint64_t)vocab + 2u * each - 2u) / each;      // pieces, wherever a row begins
+    const uint64_t chunks = (most + LP_THREADS * LP_BACK_EACH - 1u) / (LP_THREADS * LP_BACK_EACH);
+    p.chunks = (uint32_t)chunks;
+    if ((uint64_t)rows * chunks >= (1ull << 31)) return DIV_ERR_SHAPE;
+    return with_type(dtype, [&](auto* t) {
+        typedef std::remove_pointer_t<decltype(t)> XT;
+        return launch_pdl(logprob_backward_kernel<XT>, dim3((uint32_t)(rows * chunks)), LP_THREADS, 0, (cudaStream_t)cuda_stream, p);
+    });
+}
+
+}  // extern "C"

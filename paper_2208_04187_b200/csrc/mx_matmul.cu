@@ -1,0 +1,441 @@
+// Products of microscaled matrices: out[i, j] = sum over k of A[i, k] * B[j, k], both operands blobs by rows (mx.cuh), on the
+// 5th-generation tensor cores' block-scaled instructions (kind::mxf8f6f4 for e4m3, kind::mxf4 for e2m1), which take
+// the scales from tensor memory and sum in 32 bits.
+//
+// One of the operands, P, fills the 128 lanes of the accumulator, the other, S, its BN columns.  S is the operand with fewer
+// rows where those fit one tile (few tokens: the weights then fill the lanes, and the tile is as narrow as the tokens), else B.
+//
+// A CTA makes one tile of 128 x BN.  A producer thread brings stages of 128 bytes of each row, codes and scales, into a ring with
+// plain bulk copies: tiles lie in the blobs as the instruction wants them.  The issuer thread waits for a stage, has its scales
+// copied into tensor memory, issues the stage's 4 products of 32 bytes of each row, and commits; the commit hands the stage back.  The
+// columns of scales go round with the ring, so that no copy meets a product that still reads them.  Four warps then bring
+// the tile from tensor memory to the output.
+//
+// Where there are fewer tiles than SMs, the sum over k is split among the CTAs of a cluster: each sums a run of stages, leaves its tile
+// in its shared memory, and takes a share of the columns, which it adds up over the cluster in the order of the ranks (the result
+// does not depend on timing).
+//
+// Every wait is bounded (MXP_LIMIT_NS): a CTA that gives up waits for its copies, gives its tensor memory back, and
+// writes NaN for its tile.
+#include "mx.cuh"
+
+namespace divk {
+
+constexpr uint32_t MXP_THREADS = 192;             // 4 warps for the way out, the producer's, the issuer's
+constexpr uint32_t MXP_MAX_STAGES = 8;
+constexpr uint64_t MXP_LIMIT_NS = 2000000000ull;
+constexpr uint32_t MXP_SMEM = 224u * 1024u;       // of a CTA, ring and control block
+
+struct MxSide {
+    const unsigned char *codes, *scales;
+    MxShape s;
+};
+struct MxProductParams {
+    MxSide p, s;
+    void* out;
+    uint64_t ld;                 // numbers between two rows of out
+    uint32_t tiles_p;
+    uint32_t swapped;            // the lanes are columns of out
+    uint32_t out_dtype;
+    uint32_t split;              // CTAs of a cluster
+    uint32_t vec;                // out: 16-byte stores along a row
+};
+struct MxCtl {
+    uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES], done;
+    uint32_t tmem, failed;
+};
+
+template <int FMT, uint32_t BN> struct MxTile {
+    typedef MxFormat<FMT> F;
+    static constexpr uint32_t S_BLOCKS = (BN + 127u) / 128u;                  // 128-row blocks of S in a tile
+    static constexpr uint32_t P_CODES = 16384u, S_CODES = BN * 128u;
+    static constexpr uint32_t SCALES = 512u * F::ATOMS;                       // of 128 rows
+    static constexpr uint32_t STAGE_BYTES = (P_CODES + S_CODES + SCALES * (1u + S_BLOCKS) + 1023u) / 1024u * 1024u;
+    static constexpr uint32_t FIT = (MXP_SMEM - 1024u - (uint32_t)sizeof(MxCtl)) / STAGE_BYTES;
+    static constexpr uint32_t SCALE_COLUMNS = 4u * F::ATOMS * (1u + S_BLOCKS);
+    static constexpr uint32_t STAGES = FIT < MXP_MAX_STAGES ? FIT : MXP_MAX_STAGES;
+    static constexpr uint32_t SMEM = 1024u + STAGES * STAGE_BYTES + (uint32_t)sizeof(MxCtl);
+    static constexpr uint32_t NEEDED = BN + SCALE_COLUMNS * STAGES;
+    static constexpr uint32_t COLUMNS = NEEDED <= 128u ? 128u : NEEDED <= 256u ? 256u : 512u;
+    static_assert(NEEDED <= 512u && STAGES >= 2u, "tensor memory");
+    static_assert(BN == 256u || STAGES * STAGE_BYTES >= 128u * BN * 4u, "a split tile waits in the ring");
+};
+
+// shared-memory matrix descriptor: start, stride between groups of 8 rows; version 1 of the layout
+__device__ __forceinline__ uint64_t mxp_desc(uint32_t at, uint32_t group_bytes, uint64_t swizzle) {
+    return (uint64_t)((at & 0x3FFFFu) >> 4) | (uint64_t)1u << 16 | (uint64_t)(group_bytes >> 4) << 32 | 1ull << 46 | swizzle << 61;
+}
+template <int FMT>
+__device__ __forceinline__ void mxp_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    if (FMT == MX_E2M1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+            : "memory");
+}
+__device__ __forceinline__ void mxp_scales(uint32_t columns, uint64_t desc) {      // 512 bytes -> 4 columns, the same for all four quarters of the lanes
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(columns), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mxp_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void mxp_load32(uint32_t at, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void mxp_load16(uint32_t at, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(at)
+        : "memory");
+}
+// waits for a phase, at most MXP_LIMIT_NS, and not once another thread of the CTA has given up
+__device__ __forceinline__ bool mxp_wait(uint64_t* bar, uint32_t parity, MxCtl* ctl) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = now_ns();
+    for (uint32_t polls = 1;; ++polls) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((polls & 63u) == 0u && (*(volatile uint32_t*)&ctl->failed || now_ns() - t0 > MXP_LIMIT_NS)) {
+            *(volatile uint32_t*)&ctl->failed = 1u;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t local, uint32_t rank) {
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+template <typename OT>
+__device__ __forceinline__ void mxp_store_run(OT* to, const float (&v)[32], uint32_t count, bool vec) {
+    if (vec && count == 32u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = v[8 * i + k];
+            Row8<OT> r;
+            r.set(w);
+            r.store(to + 8 * i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if ((uint32_t)i < count) to[i] = from_f32<OT>(v[i]);
+    }
+}
+template <typename OT>
+__device__ __forceinline__ void mxp_out(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
+    if (row_p >= p.p.s.rows || row_s >= p.s.s.rows) return;
+    const uint32_t count = min(n, p.s.s.rows - row_s);
+    OT* out = static_cast<OT*>(p.out);
+    if (p.swapped) {
+        OT* to = out + (uint64_t)row_s * p.ld + row_p;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if ((uint32_t)i < count) to[i * p.ld] = from_f32<OT>(v[i]);
+    } else {
+        mxp_store_run(out + (uint64_t)row_p * p.ld + row_s, v, count, p.vec);
+    }
+}
+__device__ __forceinline__ void mxp_out_any(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
+    if (p.out_dtype == DIV_BF16) mxp_out<__nv_bfloat16>(p, row_p, row_s, n, v);
+    else if (p.out_dtype == DIV_F16) mxp_out<__half>(p, row_p, row_s, n, v);
+    else mxp_out<float>(p, row_p, row_s, n, v);
+}
+
+template <int FMT, uint32_t BN>
+__global__ void __launch_bounds__(MXP_THREADS, 1)
+mx_product_kernel(const __grid_constant__ MxProductParams p) {
+    typedef MxTile<FMT, BN> T;
+    typedef MxFormat<FMT> F;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    MxCtl* ctl = reinterpret_cast<MxCtl*>(ring + T::STAGES * T::STAGE_BYTES);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+
+    const uint32_t rank = p.split > 1u ? cluster_rank() : 0u, tile = blockIdx.x / p.split;
+    const uint32_t tp = tile % p.tiles_p, ts = tile / p.tiles_p;
+    const uint32_t all = p.p.s.stages;
+    const uint32_t k0 = (uint32_t)((uint64_t)all * rank / p.split), k1 = (uint32_t)((uint64_t)all * (rank + 1u) / p.split);
+    const uint32_t p0 = tp * 128u, s0 = ts * BN;
+
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem)), "n"(T::COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < T::STAGES; ++i) {
+            mbar_init(&ctl->full[i], 1);
+            mbar_init(&ctl->empty[i], 1);
+        }
+        mbar_init(&ctl->done, 1);
+        ctl->failed = 0;
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *(volatile uint32_t*)&ctl->tmem;
+    griddep_wait();
+    griddep_launch();
+
+    if (warp == 4 && lane == 0) {
+        // ---- producer ----
+        const uint32_t hp = mx_tile_rows(p.p.s, tp) * 128u;
+        // rows of S: of its only block of 128 (BN < 128), or BN / 128 whole blocks
+        uint32_t hs[T::S_BLOCKS];
+        const unsigned char* from_s[T::S_BLOCKS];
+        const unsigned char* scales_s[T::S_BLOCKS];
+        uint32_t step_s[T::S_BLOCKS];
+        uint32_t bytes = hp + T::SCALES;
+#pragma unroll
+        for (uint32_t b = 0; b < T::S_BLOCKS; ++b) {
+            const uint32_t row = s0 + b * 128u, rb = row / 128u;
+            const bool there = row < p.s.s.rows;
+            const uint32_t height = there ? mx_tile_rows(p.s.s, rb) : 0u;
+            hs[b] = min(height, BN) * 128u;
+            from_s[b] = p.s.codes + (there ? mx_tile_offset(p.s.s, rb, 0) : 0u);
+            step_s[b] = height * 128u;
+            scales_s[b] = p.s.scales + (uint64_t)(there ? rb : 0u) * p.s.s.stages * T::SCALES;
+            bytes += hs[b] + T::SCALES;                       // (scales of a block that is not there: those of the first, for columns that nobody keeps)
+        }
+        const unsigned char* from_p = p.p.codes + mx_tile_offset(p.p.s, tp, 0);
+        const unsigned char* scales_p = p.p.scales + (uint64_t)tp * all * T::SCALES;
+        uint32_t asked = 0;
+        bool ok = true;
+        for (uint32_t k = k0; k < k1 && ok; ++k, ++asked) {
+            const uint32_t slot = asked % T::STAGES, turn = asked / T::STAGES;
+            if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl)) {
+                ok = false;
+                break;
+            }
+            unsigned char* at = ring + slot * T::STAGE_BYTES;
+            uint64_t* bar = &ctl->full[slot];
+            mbar_arrive_expect_tx(bar, bytes);
+            bulk_load(at, from_p + (uint64_t)k * hp, hp, bar);
+            bulk_load(at + T::P_CODES + T::S_CODES, scales_p + (uint64_t)k * T::SCALES, T::SCALES, bar);
+#pragma unroll
+            for (uint32_t b = 0; b < T::S_BLOCKS; ++b) {
+                if (hs[b]) bulk_load(at + T::P_CODES + b * 16384u, from_s[b] + (uint64_t)k * step_s[b], hs[b], bar);
+                bulk_load(at + T::P_CODES + T::S_CODES + (1u + b) * T::SCALES, scales_s[b] + (uint64_t)k * T::SCALES, T::SCALES, bar);
+            }
+        }
+        // no copy may land after the CTA has gone, whoever gave up.  (Slots of earlier fills were handed back full.)
+        const uint64_t t0 = now_ns();
+        for (uint32_t i = asked > T::STAGES ? asked - T::STAGES : 0u; i < asked; ++i)
+            while (!mbar_try_wait(&ctl->full[i % T::STAGES], (i / T::STAGES) & 1u) && now_ns() - t0 < MXP_LIMIT_NS) {}
+    } else if (warp == 5 && lane == 0) {
+        // ---- issuer ----
+        // dense, both operands of one type, scales with 8 bits of exponent, BN columns, 128 lanes
+        const uint32_t type = FMT == MX_E2M1 ? 1u : 0u;
+        const uint32_t idesc0 = type << 7 | type << 10 | (BN >> 3) << 17 | 1u << 23 | (128u >> 4) << 24;
+        const uint32_t scales0 = tmem + BN;
+        bool ok = true;
+        for (uint32_t k = k0, n = 0; k < k1; ++k, ++n) {
+            const uint32_t slot = n % T::STAGES;
+            if (!mxp_wait(&ctl->full[slot], (n / T::STAGES) & 1u, ctl)) {
+                ok = false;
+                break;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = smem_u32(ring + slot * T::STAGE_BYTES), sc = at + T::P_CODES + T::S_CODES;
+            const uint32_t cp = scales0 + slot * T::SCALE_COLUMNS, cs = cp + 4u * F::ATOMS;
+#pragma unroll
+            for (uint32_t a = 0; a < F::ATOMS; ++a) {
+                mxp_scales(cp + 4u * a, mxp_desc(sc + 512u * a, 128u, 0));
+#pragma unroll
+                for (uint32_t b = 0; b < T::S_BLOCKS; ++b)
+                    mxp_scales(cs + 4u * (a * T::S_BLOCKS + b), mxp_desc(sc + (1u + b) * T::SCALES + 512u * a, 128u, 0));
+            }
+            const uint64_t dp = mxp_desc(at, 1024u, 2), ds = mxp_desc(at + T::P_CODES, 1024u, 2);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t atom = FMT == MX_E2M1 ? i >> 1 : 0u, id = FMT == MX_E2M1 ? (i & 1u) * 2u : i;
+                mxp_mma<FMT>(tmem, dp + 2u * i, ds + 2u * i, idesc0 | id << 4 | id << 29, cp + 4u * atom, cs + 4u * T::S_BLOCKS * atom,
+                             (n | i) != 0u);
+            }
+            mxp_commit(&ctl->empty[slot]);
+        }
+        mxp_commit(&ctl->done);
+        if (!ok) mxp_wait(&ctl->done, 0, ctl);                     // (what has been issued ends before the tensor memory goes)
+    }
+    __syncwarp();
+
+    // ---- the way out: warps 0..3, each its quarter of the lanes ----
+    bool good = true;
+    const uint32_t quarter = tmem + (warp << 21);                 // lane 32 * warp in the upper half of the address
+    const uint32_t row = warp * 32u + lane;
+    float v[32];
+    if (warp < 4) {
+        good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, 0, ctl));
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        good = good && !*(volatile uint32_t*)&ctl->failed;
+        if (p.split == 1u) {
+            for (uint32_t c = 0; c < BN; c += 32u) {
+                uint32_t raw[32];
+                __syncwarp();
+                if (BN < 32u) mxp_load16(quarter + c, raw);
+                else mxp_load32(quarter + c, raw);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = (BN >= 32u || i < 16) ? (good ? __uint_as_float(raw[i]) : __uint_as_float(0x7FC00000u)) : 0.f;
+                mxp_out_any(p, p0 + row, s0 + c, min(BN, 32u), v);
+            }
+        } else {
+            float* part = reinterpret_cast<float*>(ring);           // [column][lane]; all copies and products are through
+            for (uint32_t c = 0; c < BN; c += 32u) {
+                uint32_t raw[32];
+                __syncwarp();
+                if (BN < 32u) mxp_load16(quarter + c, raw);
+                else mxp_load32(quarter + c, raw);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (BN >= 32u || i < 16) part[(c + i) * 128u + row] = good ? __uint_as_float(raw[i]) : __uint_as_float(0x7FC00000u);
+            }
+        }
+    }
+    if (p.split > 1u) {
+        cluster_sync_all();
+        if (warp < 4) {
+            const uint32_t share = BN / p.split, c0 = rank * share;        // (a power of two of at least 2)
+            const uint32_t mine = smem_u32(ring) + (c0 * 128u + row) * 4u;
+            for (uint32_t c = 0; c < share; c += 32u) {
+                const uint32_t n = min(share - c, 32u);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    float sum = 0.f;
+                    if ((uint32_t)i < n && s0 + c0 + c + i < p.s.s.rows)
+                        for (uint32_t r = 0; r < p.split; ++r) sum += ld_cluster(mine + (c + i) * 512u, r);
+                    v[i] = sum;
+                }
+                mxp_out_any(p, p0 + row, s0 + c0 + c, n, v);
+            }
+        }
+        cluster_sync_all();                                                // nobody leaves while another reads here
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 5) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(T::COLUMNS));
+    }
+}
+
+}  // namespace divk
+
+namespace {
+using namespace divk;
+
+template <int FMT, uint32_t BN>
+div_status product_launch(const MxProductParams& p, uint32_t grid, cudaStream_t st) {
+    typedef MxTile<FMT, BN> T;
+    auto kern = mx_product_kernel<FMT, BN>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)T::SMEM) != cudaSuccess) {
+        cudaGetLastError();
+        return DIV_ERR_CUDA;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(MXP_THREADS);
+    cfg.dynamicSmemBytes = T::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = p.split;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, kern, p) != cudaSuccess) {
+        cudaGetLastError();
+        return DIV_ERR_CUDA;
+    }
+    return DIV_OK;
+}
+
+template <int FMT>
+div_status product_by_width(uint32_t bn, const MxProductParams& p, uint32_t grid, cudaStream_t st) {
+    switch (bn) {
+        case 16: return product_launch<FMT, 16>(p, grid, st);
+        case 32: return product_launch<FMT, 32>(p, grid, st);
+        case 64: return product_launch<FMT, 64>(p, grid, st);
+        case 128: return product_launch<FMT, 128>(p, grid, st);
+    }
+    return product_launch<FMT, 256>(p, grid, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
+                         void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream) {
+    if (!a_dev || !b_dev || !out_dev) return DIV_ERR_NULL;
+    if (!lm_size_ok(m) || !lm_size_ok(n) || !lm_size_ok(k) || (m > 1 && out_row_stride < n)) return DIV_ERR_SHAPE;
+    if (!lm_dtype_ok(out_dtype) || !mx_format_ok(format)) return DIV_ERR_PARAM;
+    const uint32_t size = lm_dtype_bytes(out_dtype);
+    if (!aligned_16(a_dev) || !aligned_16(b_dev) || reinterpret_cast<uintptr_t>(out_dev) % size != 0) return DIV_ERR_ALIGN;
+    MxSide a, b;
+    a.s = mx_shape((uint32_t)m, (uint32_t)k, format);
+    b.s = mx_shape((uint32_t)n, (uint32_t)k, format);
+    if (a_bytes < mx_codes_bytes(a.s) + mx_scales_bytes(a.s, format) || b_bytes < mx_codes_bytes(b.s) + mx_scales_bytes(b.s, format)) return DIV_ERR_CAPACITY;
+    a.codes = (const unsigned char*)a_dev;
+    a.scales = a.codes + mx_scales_at(a.s);
+    b.codes = (const unsigned char*)b_dev;
+    b.scales = b.codes + mx_scales_at(b.s);
+
+    MxProductParams p;
+    const bool swapped = m < n && m <= 64;
+    p.p = swapped ? b : a;
+    p.s = swapped ? a : b;
+    p.swapped = swapped;
+    p.out = out_dev;
+    p.ld = (uint64_t)out_row_stride;
+    p.out_dtype = (uint32_t)out_dtype;
+    p.vec = aligned_16(out_dev) && (m == 1 || out_row_stride * size % 16 == 0);
+    const uint64_t rows_s = p.s.s.rows;
+    p.tiles_p = (p.p.s.rows + 127u) / 128u;
+    uint32_t bn = rows_s <= 16 ? 16u : rows_s <= 32 ? 32u : rows_s <= 64 ? 64u : 128u;
+    if (bn == 128u && (uint64_t)p.tiles_p * ((rows_s + 255u) / 256u) >= 120u) bn = 256u;
+    const uint64_t tiles = p.tiles_p * ((rows_s + bn - 1u) / bn);
+    uint32_t split = 1;
+    while (bn < 256u && split < 8u && tiles * split * 2u <= 160u && p.p.s.stages >= 4u * split) split *= 2u;
+    p.split = split;
+    if (tiles * split >= (1ull << 31)) return DIV_ERR_SHAPE;
+    return format == MX_E4M3 ? product_by_width<MX_E4M3>(bn, p, (uint32_t)(tiles * split), (cudaStream_t)cuda_stream)
+                             : product_by_width<MX_E2M1>(bn, p, (uint32_t)(tiles * split), (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,376 @@
+"""Operators of language models on torch tensors: matrices held in microscaled 8- or 4-bit numbers and their products, the
+root-mean-square norm that feeds them, and log probabilities of given tokens.
+
+What the activation codec does for feature maps these do for the layers of a transformer: what a linear layer keeps for its
+backward pass is the quantised form of its input, 8.25 or 4.25 bits a number, and the products take that form as it is.
+
+    q = mx_quantize(w, "e2m1")                        # weights, laid out once
+    y = mx_matmul(mx_quantize(x, "e2m1"), q, x.dtype) # inference
+    y = mx_linear(x, w)                               # training: gradients of x and w from quantised operands
+    y, h = rms_norm(x, g, residual)                   # h = x + residual, y = its norm; gradients
+    q, h = rms_norm_mx(x, g, residual)                # inference: y in 8 bits, what mx_matmul takes
+    logprobs, entropy, top, indices = token_logprobs(logits, targets, top=5)
+
+`DivisionLinear`, `DivisionRMSNorm` and `DivisionNormLinear` are the modules; `to_division_layers` puts them in place of torch's.
+
+Glue only, as in `autograd`: every step runs in the CUDA library through the C ABI (include/division.h says what it
+computes), on the current stream of the inputs' device.  Inputs are CUDA tensors of dtype float32, bfloat16 or float16; leading
+dimensions are folded into rows.  Rows that are runs of neighbours are read where they are, whatever their stride.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple
+
+import torch
+
+from . import binding
+
+_FORMATS = binding.MX_FORMATS
+
+
+def _format(fmt: str) -> int:
+    try:
+        return _FORMATS[fmt]
+    except KeyError:
+        raise ValueError(f"fmt must be one of {tuple(_FORMATS)}, not {fmt!r}") from None
+
+
+def _call(name: str, *args):
+    got = getattr(binding._native or binding.native(), name)(*args)
+    if got.__class__ is int:
+        raise binding.DivisionError(got, "div_" + name)
+    return got
+
+
+class MxTensor:
+    """A matrix in microscaled numbers: rows x cols, blocks of 32 neighbours along a row with one scale each."""
+    __slots__ = ("blob", "rows", "cols", "fmt")
+
+    def __init__(self, blob, rows: int, cols: int, fmt: str):
+        self.blob, self.rows, self.cols, self.fmt = blob, rows, cols, fmt
+
+    @property
+    def shape(self):
+        return torch.Size((self.rows, self.cols))
+
+    @property
+    def device(self):
+        return self.blob.device
+
+    @property
+    def nbytes(self) -> int:
+        """Bytes of the codes and scales themselves (the blob is a little larger: whole tiles)."""
+        return int(binding.div_mx_bytes(self.rows, self.cols, self.fmt).closed_form_bytes) if self.rows else 0
+
+    def dequantize(self, dtype=torch.bfloat16):
+        """The numbers it stands for (exact in bfloat16 and float32)."""
+        if self.rows == 0:
+            return torch.empty(0, self.cols, dtype=dtype, device=self.blob.device)
+        return _call("mx_dequantize", self.blob, self.rows, self.cols, _FORMATS[self.fmt], dtype)
+
+    def __repr__(self):
+        return f"MxTensor({self.rows} x {self.cols}, {self.fmt}, {self.blob.device})"
+
+
+def _matrix(x, what="x"):
+    if not isinstance(x, torch.Tensor) or x.dim() < 1:
+        raise ValueError(f"{what} must be a tensor of at least one dimension")
+    if x.shape[-1] == 0:
+        raise ValueError(f"{what} has rows of no numbers")
+    return x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+
+
+def _empty(x, fmt):
+    return MxTensor(torch.empty(0, dtype=torch.uint8, device=x.device), 0, x.shape[1], fmt)
+
+
+def mx_quantize(x, fmt: str = "e4m3") -> MxTensor:
+    """x (leading dimensions folded) quantised by rows: blocks along the last dimension.  No gradient passes."""
+    code, x = _format(fmt), _matrix(x)
+    if x.shape[0] == 0:
+        return _empty(x, fmt)
+    return MxTensor(_call("mx_quantize", x, code, True, False)[0], x.shape[0], x.shape[1], fmt)
+
+
+def mx_quantize_both(x, fmt: str = "e4m3"):
+    """(x by rows, its transpose by rows) from one reading: what the forward product takes, and what the gradient of the
+    weights takes, whose sum runs over the rows of x.  No gradient passes."""
+    code, x = _format(fmt), _matrix(x)
+    if x.shape[0] == 0:
+        raise ValueError("x has no rows")
+    rows, columns = _call("mx_quantize", x, code, True, True)
+    return MxTensor(rows, x.shape[0], x.shape[1], fmt), MxTensor(columns, x.shape[1], x.shape[0], fmt)
+
+
+def mx_quantize_columns(x, fmt: str = "e4m3") -> MxTensor:
+    """The transpose of x quantised by rows."""
+    code, x = _format(fmt), _matrix(x)
+    if x.shape[0] == 0:
+        raise ValueError("x has no rows")
+    return MxTensor(_call("mx_quantize", x, code, False, True)[1], x.shape[1], x.shape[0], fmt)
+
+
+def mx_matmul(a: MxTensor, b: MxTensor, dtype=torch.bfloat16):
+    """a @ b.T of two matrices with rows of equal length and one format; sums in 32 bits, rounded to dtype once."""
+    if not isinstance(a, MxTensor) or not isinstance(b, MxTensor):
+        raise ValueError("mx_matmul takes two MxTensors")
+    if a.fmt != b.fmt or a.cols != b.cols:
+        raise ValueError(f"operands differ in format or length of rows: {a!r}, {b!r}")
+    if a.rows == 0 or b.rows == 0:
+        return torch.empty(a.rows, b.rows, dtype=dtype, device=a.device)
+    return _call("mx_matmul", a.blob, a.rows, b.blob, b.rows, a.cols, _FORMATS[a.fmt], dtype)
+
+
+class _MxLinear(torch.autograd.Function):
+    """y = Q(x) Q(w)^T, dx = Q(dy) Q(w^T)^T, dw = Q(dy^T) Q(x^T)^T; kept for backward: x and w by columns."""
+
+    @staticmethod
+    def forward(ctx, x, w, fmt):
+        need_x, need_w = ctx.needs_input_grad[:2]
+        if need_w:
+            xr, ctx.xc = mx_quantize_both(x, fmt)
+        else:
+            xr, ctx.xc = mx_quantize(x, fmt), None
+        if need_x:
+            wr, ctx.wc = mx_quantize_both(w, fmt)
+        else:
+            wr, ctx.wc = mx_quantize(w, fmt), None
+        ctx.fmt, ctx.types = fmt, (x.dtype, w.dtype)
+        return mx_matmul(xr, wr, x.dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx = dw = None
+        if ctx.wc is not None and ctx.xc is not None:
+            rows, columns = mx_quantize_both(dy, ctx.fmt)
+        elif ctx.wc is not None:
+            rows = mx_quantize(dy, ctx.fmt)
+        else:
+            columns = mx_quantize_columns(dy, ctx.fmt)
+        if ctx.wc is not None:
+            dx = mx_matmul(rows, ctx.wc, ctx.types[0])
+        if ctx.xc is not None:
+            dw = mx_matmul(columns, ctx.xc, ctx.types[1])
+        return dx, dw, None
+
+
+def _check_weight(x, w):
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != x.shape[-1] or w.shape[0] == 0:
+        raise ValueError("the weight must be a matrix with one column for each feature of x")
+    if w.device != x.device:
+        raise ValueError("x and the weight must be on one device")
+
+
+def mx_linear(x, w, fmt: str = "e4m3"):
+    """x @ w.T with both operands quantised, blocks of 32 along the features; the gradients of x and w come from quantised
+    operands too, their blocks along what each product sums over (straight through the rounding).  The result has x's dtype."""
+    _format(fmt)
+    flat = _matrix(x)
+    _check_weight(x, w)
+    if flat.shape[0] == 0:
+        return flat.new_empty(*x.shape[:-1], w.shape[0]) + 0 * (flat.sum() + w.sum()).to(x.dtype)      # no rows: gradients are 0
+    y = _MxLinear.apply(flat, w, fmt)
+    return y if x.dim() == 2 else y.view(*x.shape[:-1], w.shape[0])
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, w, eps):
+        y, _, h, rstd = _call("rms_norm_forward", x, residual, w, eps, True, -1, True)
+        ctx.fused = residual is not None
+        ctx.save_for_backward(x if h is None else h, w, rstd)
+        ctx.set_materialize_grads(False)
+        return (y, h) if ctx.fused else y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, w, rstd = ctx.saved_tensors
+        if dy is None:
+            return dh, dh if ctx.fused else None, None, None
+        dx, dw = _call("rms_norm_backward", dy, dh, h, w, rstd, ctx.needs_input_grad[2])
+        return dx, dx if ctx.fused else None, dw, None
+
+
+def _norm_args(x, w, residual):
+    flat = _matrix(x)
+    if residual is not None:
+        if not isinstance(residual, torch.Tensor) or residual.shape != x.shape:
+            raise ValueError("residual must have the shape of x")
+        residual = _matrix(residual, "residual")
+    return flat, residual
+
+
+def rms_norm(x, weight, residual=None, eps: float = 1e-6):
+    """(y, h): h = x + residual rounded to x's dtype (x itself without a residual), y = h / sqrt(mean(h^2) + eps) * weight over the last
+    dimension.  weight: x's dtype or float32.  Differentiable in x, residual and weight."""
+    flat, res = _norm_args(x, weight, residual)
+    if flat.shape[0] == 0:
+        h = x if residual is None else x + residual
+        return (h * weight).to(x.dtype), h
+    if res is None:
+        return _RmsNorm.apply(flat, None, weight, float(eps)).view(x.shape), x
+    y, h = _RmsNorm.apply(flat, res, weight, float(eps))
+    return y.view(x.shape), h.view(x.shape)
+
+
+def rms_norm_mx(x, weight, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
+    """(q, h): as rms_norm, with y handed on as an MxTensor (rows folded), quantised from its 32-bit values.  No gradient passes."""
+    code = _format(fmt)
+    flat, res = _norm_args(x, weight, residual)
+    if flat.shape[0] == 0:
+        return _empty(flat, fmt), x if residual is None else x + residual
+    _, blob, h, _ = _call("rms_norm_forward", flat, res, weight, float(eps), False, code, False)
+    return MxTensor(blob, flat.shape[0], flat.shape[1], fmt), x if h is None else h.view(x.shape)
+
+
+class _MxNormLinear(torch.autograd.Function):
+    """The norm's 8- or 4-bit output goes straight into the product; kept for backward: h and rstd, from which the product's
+    input is made again, and the weight's columns."""
+
+    @staticmethod
+    def forward(ctx, x, residual, g, w, eps, fmt):
+        _, blob, h, rstd = _call("rms_norm_forward", x, residual, g, eps, False, _FORMATS[fmt], True)
+        wr, ctx.wc = mx_quantize_both(w, fmt)
+        out = mx_matmul(MxTensor(blob, x.shape[0], x.shape[1], fmt), wr, x.dtype)
+        ctx.fmt, ctx.eps, ctx.fused, ctx.w_dtype = fmt, eps, residual is not None, w.dtype
+        ctx.save_for_backward(x if h is None else h, g, rstd)
+        ctx.set_materialize_grads(False)
+        return (out, h) if ctx.fused else out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dh=None):
+        h, g, rstd = ctx.saved_tensors
+        if dout is None:
+            return dh, dh if ctx.fused else None, None, None, None, None
+        rows, columns = mx_quantize_both(dout, ctx.fmt)
+        dw = None
+        if ctx.needs_input_grad[3]:
+            y = _call("rms_norm_forward", h, None, g, ctx.eps, True, -1, False)[0]
+            dw = mx_matmul(columns, mx_quantize_columns(y, ctx.fmt), ctx.w_dtype)
+        dy = mx_matmul(rows, ctx.wc, h.dtype)
+        dx, dg = _call("rms_norm_backward", dy, dh, h, g, rstd, ctx.needs_input_grad[2])
+        return dx, dx if ctx.fused else None, dg, dw, None, None
+
+
+def mx_norm_linear(x, norm_weight, w, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
+    """(mx_linear of the norm, h) with nothing kept of the norm's output: (out, h) as of rms_norm and mx_linear."""
+    _format(fmt)
+    flat, res = _norm_args(x, norm_weight, residual)
+    _check_weight(x, w)
+    if flat.shape[0] == 0:
+        y, h = rms_norm(x, norm_weight, residual, eps)
+        return mx_linear(y, w, fmt), h
+    got = _MxNormLinear.apply(flat, res, norm_weight, w, float(eps), fmt)
+    out, h = got if res is not None else (got, flat)
+    return out.view(*x.shape[:-1], w.shape[0]), h.view(x.shape)
+
+
+class TokenLogprobs(NamedTuple):
+    logprobs: torch.Tensor
+    entropy: torch.Tensor
+    top_logprobs: torch.Tensor
+    top_indices: torch.Tensor
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, top):
+        logprobs, entropy, stats, top_logprobs, top_indices = _call("token_logprobs_forward", logits, targets, top)
+        ctx.save_for_backward(logits, targets, stats, entropy)
+        ctx.mark_non_differentiable(top_logprobs, top_indices)
+        ctx.set_materialize_grads(False)
+        return logprobs, entropy, top_logprobs, top_indices
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogprobs, dentropy, _top, _indices):
+        logits, targets, stats, entropy = ctx.saved_tensors
+        if dlogprobs is None and dentropy is None:
+            return None, None, None
+        return _call("token_logprobs_backward", logits, targets, stats, entropy, dlogprobs, dentropy), None, None
+
+
+def token_logprobs(logits, targets, top: int = 0) -> TokenLogprobs:
+    """Log probabilities of `targets` (int64, one a row; negative: none, 0) under softmax(logits), the entropies, and the `top` (at most
+    32) most probable tokens with theirs, equal ones by index.  logits: ... x vocabulary.  Results in float32.  The logits are all that
+    is kept for the backward pass, beside four numbers a row; log probabilities and entropies are differentiable, the alternatives
+    are not."""
+    flat = _matrix(logits, "logits")
+    if not isinstance(targets, torch.Tensor) or targets.shape != logits.shape[:-1]:
+        raise ValueError("targets must have the shape of logits without the last dimension")
+    top = int(top)
+    if flat.shape[0] == 0:
+        if not 0 <= top <= min(32, flat.shape[1]):
+            raise ValueError("top must lie between 0 and 32 and not pass the vocabulary")
+        none = flat.sum(-1).float()
+        return TokenLogprobs(none.view(targets.shape), none.clone().view(targets.shape), none.new_empty(*targets.shape, top),
+                             targets.new_empty(*targets.shape, top))
+    got = _TokenLogprobs.apply(flat, targets.reshape(-1), top)
+    if logits.dim() == 2:
+        return TokenLogprobs(*got)
+    return TokenLogprobs(got[0].view(targets.shape), got[1].view(targets.shape), got[2].view(*targets.shape, top), got[3].view(*targets.shape, top))
+
+
+# ------------------------------------------------------------------------------------------------------------
+# modules
+# ------------------------------------------------------------------------------------------------------------
+class DivisionLinear(torch.nn.Linear):
+    """nn.Linear whose products take quantised operands; what it keeps of its input has 8 or 4 bits a number."""
+
+    def __init__(self, in_features, out_features, bias=True, fmt: str = "e4m3", device=None, dtype=None):
+        super().__init__(in_features, out_features, bias, device, dtype)
+        _format(fmt)
+        self.fmt = fmt
+
+    def forward(self, x):
+        y = mx_linear(x, self.weight, self.fmt)
+        return y if self.bias is None else y + self.bias.to(y.dtype)
+
+
+class DivisionRMSNorm(torch.nn.Module):
+    """rms_norm with its weight; with a residual it returns (y, h)."""
+
+    def __init__(self, features, eps: float = 1e-6, device=None, dtype=None):
+        super().__init__()
+        self.weight, self.eps = torch.nn.Parameter(torch.ones(features, device=device, dtype=dtype)), eps
+
+    def forward(self, x, residual=None):
+        y, h = rms_norm(x, self.weight, residual, self.eps)
+        return y if residual is None else (y, h)
+
+
+class DivisionNormLinear(torch.nn.Module):
+    """A norm and the linear layer behind it, without a bias; with a residual it returns (out, h)."""
+
+    def __init__(self, in_features, out_features, eps: float = 1e-6, fmt: str = "e4m3", device=None, dtype=None):
+        super().__init__()
+        _format(fmt)
+        self.norm_weight = torch.nn.Parameter(torch.ones(in_features, device=device, dtype=dtype))
+        self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device, dtype=dtype))
+        torch.nn.init.kaiming_uniform_(self.weight, a=5 ** 0.5)
+        self.eps, self.fmt = eps, fmt
+
+    def forward(self, x, residual=None):
+        out, h = mx_norm_linear(x, self.norm_weight, self.weight, residual, self.eps, self.fmt)
+        return out if residual is None else (out, h)
+
+
+def to_division_layers(module: torch.nn.Module, fmt: str = "e4m3") -> torch.nn.Module:
+    """Replace every nn.Linear in `module` by DivisionLinear and every nn.RMSNorm over one dimension by DivisionRMSNorm, with their
+    parameters (in place; returns the module)."""
+    for name, child in list(module.named_children()):
+        if type(child) is torch.nn.Linear:
+            new = DivisionLinear(child.in_features, child.out_features, child.bias is not None, fmt, device="meta")
+            new.weight, new.bias = child.weight, child.bias
+            setattr(module, name, new.train(child.training))
+        elif type(child) is torch.nn.RMSNorm and len(child.normalized_shape) == 1 and child.weight is not None:
+            eps = torch.finfo(child.weight.dtype).eps if child.eps is None else child.eps
+            new = DivisionRMSNorm(child.normalized_shape[0], eps, device="meta")
+            new.weight = child.weight
+            setattr(module, name, new.train(child.training))
+        else:
+            to_division_layers(child, fmt)
+    return module

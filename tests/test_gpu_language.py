@@ -1,0 +1,182 @@
+"""The operators of language models as they are used together: layers, a small model's training step, a captured decoding
+step."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import language_oracle as lo
+from paper_2208_04187_b200 import build
+from paper_2208_04187_b200 import language as lm
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built_library():
+    build.build()
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def make(*shape, seed=0, scale=1.0, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed)
+    return (scale * torch.randn(*shape, generator=g)).to(dtype)
+
+
+def near(got, a, b, dtype):
+    """A product of quantised operands: sums in 32 bits, one rounding."""
+    want, size = a @ b.T, np.abs(a) @ np.abs(b).T
+    half = torch.finfo(dtype).eps / 2
+    bound = a.shape[1] * 2.0 ** -23 * size
+    assert (np.abs(f64(got) - want) <= bound + half * (np.abs(want) + bound)).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("m, k, n", [(1, 64, 96), (37, 100, 130), (256, 384, 128), (500, 65, 33)])
+def test_linear_and_its_gradients(m, k, n, fmt):
+    x, w, dy = make(m, k, seed=1), make(n, k, seed=2, dtype=torch.float32), make(m, n, seed=3)
+    xd, wd = x.cuda().requires_grad_(), w.cuda().requires_grad_()
+    y = lm.mx_linear(xd, wd, fmt=fmt)
+    q = lambda a: lo.mx_values(a, fmt)  # noqa: E731
+    near(y, q(f64(x)), q(f64(w)), torch.bfloat16)
+    dx, dw = torch.autograd.grad(y, (xd, wd), dy.cuda(), retain_graph=True)
+    assert dx.dtype == torch.bfloat16 and dw.dtype == torch.float32
+    near(dx, q(f64(dy)), q(f64(w).T), torch.bfloat16)
+    near(dw, q(f64(dy).T), q(f64(x).T), torch.float32)
+    # one of them alone
+    assert torch.equal(torch.autograd.grad(lm.mx_linear(xd, w.cuda(), fmt=fmt), xd, dy.cuda())[0], dx)
+    assert torch.equal(torch.autograd.grad(lm.mx_linear(x.cuda(), wd, fmt=fmt), wd, dy.cuda())[0], dw)
+    three = lm.mx_linear(xd.view(m, 1, k), wd, fmt=fmt)
+    assert torch.equal(three.view(m, n), y)
+
+
+def test_what_a_linear_layer_keeps():
+    x = make(4096, 2048, seed=1).cuda().requires_grad_()
+    w = make(2048, 2048, seed=2).cuda().requires_grad_()
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    y = lm.mx_linear(x, w, fmt="e2m1")
+    kept = torch.cuda.memory_allocated() - before - y.numel() * 2
+    assert kept <= (x.numel() + w.numel()) * 4.25 / 8 * 1.02
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("fused", [False, True])
+def test_norm_and_linear_in_one(fmt, fused):
+    x, r, g, w = make(70, 200, seed=1).cuda(), make(70, 200, seed=2).cuda(), (1 + make(200, seed=3, scale=0.1)).cuda(), make(150, 200, seed=4).cuda()
+    args = [t.requires_grad_() for t in (x, g, w)] + ([r.requires_grad_()] if fused else [])
+    out, h = lm.mx_norm_linear(x, g, w, r if fused else None, eps=1e-5, fmt=fmt)
+    q, h2 = lm.rms_norm_mx(x, g, r if fused else None, eps=1e-5, fmt=fmt)
+    assert torch.equal(h, h2) and torch.equal(out, lm.mx_matmul(q, lm.mx_quantize(w, fmt)))
+    do, dh = make(70, 150, seed=5).cuda(), make(70, 200, seed=6).cuda()
+    got = torch.autograd.grad((out, h) if fused else out, args, (do, dh) if fused else do)
+    # the same from its parts
+    y, h3 = lm.rms_norm(x, g, r if fused else None, eps=1e-5)
+    dy = lm.mx_matmul(lm.mx_quantize(do, fmt), lm.mx_quantize_columns(w, fmt))
+    parts = torch.autograd.grad((y, h3) if fused else y, [args[0], args[1]] + args[3:], (dy, dh) if fused else dy)
+    assert torch.equal(got[0], parts[0]) and torch.equal(got[1], parts[1])
+    assert torch.equal(got[2], lm.mx_matmul(lm.mx_quantize_columns(do, fmt), lm.mx_quantize_columns(y, fmt)))
+    if fused:
+        assert torch.equal(got[3], parts[2])
+
+
+class Block(torch.nn.Module):
+    def __init__(self, d, fmt):
+        super().__init__()
+        self.up = lm.DivisionNormLinear(d, 2 * d, fmt=fmt, device="cuda", dtype=torch.bfloat16)
+        self.down = lm.DivisionLinear(2 * d, d, fmt=fmt, device="cuda", dtype=torch.bfloat16)
+
+    def forward(self, x, h):
+        out, h = self.up(x, h)
+        return self.down(torch.relu(out)), h
+
+
+class Model(torch.nn.Module):
+    def __init__(self, vocab, d, layers, fmt):
+        super().__init__()
+        self.embed = torch.nn.Embedding(vocab, d, device="cuda", dtype=torch.bfloat16)
+        self.blocks = torch.nn.ModuleList(Block(d, fmt) for _ in range(layers))
+        self.norm = lm.DivisionRMSNorm(d, device="cuda", dtype=torch.bfloat16)
+        self.head = lm.DivisionLinear(d, vocab, bias=False, fmt=fmt, device="cuda", dtype=torch.bfloat16)
+
+    def forward(self, tokens):
+        h = self.embed(tokens)
+        x = torch.zeros_like(h)
+        for b in self.blocks:
+            x, h = b(x, h)
+        y, _ = self.norm(x, h)
+        return self.head(y)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+def test_a_training_step(fmt):
+    torch.manual_seed(0)
+    model = Model(501, 96, 2, fmt)
+    tokens = torch.randint(0, 501, (4, 33), device="cuda")
+    got = lm.token_logprobs(model(tokens[:, :-1]), tokens[:, 1:])
+    loss = -got.logprobs.mean() - 0.01 * got.entropy.mean()
+    loss.backward()
+    grads = [p.grad for p in model.parameters()]
+    assert all(g is not None and g.shape == p.shape and g.isfinite().all() and g.abs().sum() > 0 for g, p in zip(grads, model.parameters()))
+    # and again, to the bit (embeddings are summed by torch in no fixed order)
+    model.zero_grad()
+    got = lm.token_logprobs(model(tokens[:, :-1]), tokens[:, 1:])
+    (-got.logprobs.mean() - 0.01 * got.entropy.mean()).backward()
+    assert all(torch.equal(a, p.grad) for a, (name, p) in zip(grads, model.named_parameters()) if "embed" not in name)
+
+
+def test_the_gradient_of_a_model_is_near_that_of_the_same_model_in_full_precision():
+    """Quantisation errors are at most half a step: 2^-4 of a number's block's largest with e4m3 (2^-4 of the number itself where it is
+    normal).  The product of two such operands is off by less than 2 * 2^-4 + 2^-8 of the sum of magnitudes."""
+    x, w = make(64, 256, seed=1), make(80, 256, seed=2)
+    y = lm.mx_linear(x.cuda(), w.cuda())
+    want, size = f64(x) @ f64(w).T, np.abs(f64(x)) @ np.abs(f64(w)).T
+    assert (np.abs(f64(y) - want) <= (2 * 2.0 ** -4 + 2.0 ** -8) * size * (1 + 2.0 ** -8) + 2.0 ** -9 * np.abs(want) + 0.05).all()
+
+
+def test_a_decoding_step_is_captured_and_replayed():
+    """Norm -> 4-bit product -> log probabilities, for one token, on buffers whose contents change."""
+    d, vocab = 512, 3000
+    g = torch.ones(d, device="cuda", dtype=torch.bfloat16)
+    w = lm.mx_quantize(make(vocab, d, seed=1).cuda(), "e2m1")
+    x, h = make(1, d, seed=2).cuda(), make(1, d, seed=3).cuda()
+    target = torch.tensor([17], device="cuda")
+
+    def step():
+        q, k = lm.rms_norm_mx(x, g, h, fmt="e2m1")
+        return (k, *lm.token_logprobs(lm.mx_matmul(q, w), target, top=8))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in range(3):
+        x.copy_(make(1, d, seed=10 + seed).cuda())
+        h.copy_(make(1, d, seed=20 + seed).cuda())
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_two_streams_at_once():
+    xs = [make(300, 1024, seed=i).cuda() for i in range(4)]
+    w = lm.mx_quantize(make(700, 1024, seed=9).cuda(), "e4m3")
+    g = torch.ones(1024, device="cuda", dtype=torch.bfloat16)
+    t = torch.arange(300, device="cuda")
+
+    def chain(x):
+        q, _ = lm.rms_norm_mx(x, g)
+        return lm.token_logprobs(lm.mx_matmul(q, w), t, top=3)
+    want = [chain(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(5):
+        got = []
+        for x, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                got.append(chain(x))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for p, q in zip(got, want) for a, b in zip(p, q))

@@ -1,0 +1,190 @@
+"""Microscaled matrices on the GPU: quantising equals the 64-bit statement number for number, products keep to what sums in
+32 bits allow."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import language_oracle as lo
+from paper_2208_04187_b200 import binding, build
+from paper_2208_04187_b200 import language as lm
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+FORMATS = ["e4m3", "e2m1"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built_library():
+    build.build()
+
+
+def matrix(rows, cols, dtype, seed=0, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g) * torch.exp(spread * torch.randn(rows, 1, generator=g))
+    x[torch.rand(rows, cols, generator=g) < 0.05] = 0
+    return x.to(TYPES[dtype])
+
+
+def same(got, want):
+    np.testing.assert_array_equal(got.cpu().double().numpy() + 0.0, want + 0.0)
+
+
+SIZES = [(1, 1), (1, 31), (3, 32), (8, 33), (9, 64), (127, 96), (128, 128), (129, 127), (1, 5000), (31, 256), (257, 384), (300, 513)]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, cols", SIZES)
+def test_quantising_by_rows_and_columns(rows, cols, dtype, fmt):
+    x = matrix(rows, cols, dtype, rows * 1000 + cols)
+    want, turned = lo.mx_values(x.double().numpy(), fmt), lo.mx_values(x.double().numpy().T, fmt)
+    xd = x.cuda()
+    a, b = lm.mx_quantize_both(xd, fmt)
+    assert a.shape == (rows, cols) and b.shape == (cols, rows)
+    same(a.dequantize(torch.float32), want)
+    same(b.dequantize(torch.float32), turned)
+    same(lm.mx_quantize(xd, fmt).dequantize(torch.bfloat16), want)              # (exact there too)
+    same(lm.mx_quantize_columns(xd, fmt).dequantize(torch.float32), turned)
+    same(lm.mx_quantize(xd.t(), fmt).dequantize(torch.float32), turned)         # a transposed matrix, read where it is
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_strides_and_alignment(fmt):
+    big = matrix(70, 700, "bf16", 5).cuda()
+    for x in (big[:, :640], big[3:, 8:72], big[:, 1:130], big[::2, :128], big[5:6, 3:40], big[:1].expand(4, 700), big.t()[5:300, :33], big.view(70, 7, 100)[:, 2]):
+        q = lm.mx_quantize(x, fmt)
+        same(q.dequantize(torch.float32), lo.mx_values(x.cpu().double().numpy(), fmt))
+        _, c = lm.mx_quantize_both(x, fmt)
+        same(c.dequantize(torch.float32), lo.mx_values(x.cpu().double().numpy().T, fmt))
+    three = lm.mx_quantize(big.view(7, 10, 700), fmt)
+    assert three.shape == (70, 700)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_extremes(fmt):
+    inf, nan = float("inf"), float("nan")
+    x = torch.zeros(12, 64)
+    x[0, 3] = inf
+    x[1, 40] = nan
+    x[2, :] = torch.linspace(-3.4e38, 3.4e38, 64)
+    x[3, :32] = 1e-45
+    x[4, :] = torch.logspace(-45, 38, 64)
+    x[5, :] = 2.0 ** -130
+    x[6, :4] = torch.tensor([448.0, 449, -448, 1e-3])
+    x[7, :4] = torch.tensor([6.0, 6.0000005, -6, 0.25])
+    x[8, :3] = torch.tensor([-inf, inf, nan])
+    x[9, :] = -0.0
+    x[10, :] = torch.finfo(torch.float32).tiny
+    x[11, 32:] = torch.finfo(torch.float32).min
+    a, b = lm.mx_quantize_both(x.cuda(), fmt)
+    same(a.dequantize(torch.float32), lo.round_to(lo.mx_values(x.double().numpy(), fmt), "f32"))
+    same(b.dequantize(torch.float32), lo.round_to(lo.mx_values(x.double().numpy().T, fmt), "f32"))
+    for t in ("bf16", "f16"):
+        y = x.clamp(-60000, 60000).to(TYPES[t])
+        same(lm.mx_quantize(y.cuda(), fmt).dequantize(torch.float32), lo.round_to(lo.mx_values(y.double().numpy(), fmt), "f32"))
+
+
+def test_rounding_back_to_half_precision():
+    x = torch.tensor([[70000.0, 1.0, -1e-9] + [0.0] * 29])
+    got = lm.mx_quantize(x.cuda(), "e4m3").dequantize(torch.float16).cpu()
+    assert torch.equal(got, torch.from_numpy(lo.mx_values(x.double().numpy(), "e4m3")).half())
+
+
+def product(a, b):
+    """(a b^T, the sum of the magnitudes) in 64 bits."""
+    return a @ b.T, np.abs(a) @ np.abs(b).T
+
+
+def check_product(y, a, b, dtype):
+    # a sum of k products in 32 bits, in any order, with additions that may cut off: k steps of 2^-23 of the magnitudes; then one rounding
+    want, size = product(a, b)
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    bound = a.shape[1] * 2.0 ** -23 * size + half * np.abs(want) * (1 + 2.0 ** -10) + (2.0 ** -25 if dtype == "f16" else 0)
+    got = y.cpu().double().numpy()
+    assert got.shape == want.shape and (np.abs(got - want) <= bound).all()
+
+
+PRODUCTS = [(1, 1, 1), (1, 128, 32), (1, 300, 4096), (2, 129, 96), (15, 256, 160), (16, 100, 512), (17, 640, 1024), (33, 1000, 300), (64, 65, 2050), (65, 64, 64),
+            (100, 100, 100), (128, 128, 256), (129, 257, 385), (300, 20, 77), (513, 1, 40), (700, 513, 288), (200, 1100, 8192), (2300, 2200, 200), (5000, 16, 64)]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m, n, k", PRODUCTS)
+def test_products(m, n, k, fmt):
+    dtype = ("f32", "bf16", "f16")[(m + n + k) % 3]
+    a, b = matrix(m, k, "bf16", m, 0.5), matrix(n, k, "f32", n + 1, 0.5)
+    y = lm.mx_matmul(lm.mx_quantize(a.cuda(), fmt), lm.mx_quantize(b.cuda(), fmt), TYPES[dtype])
+    assert y.dtype == TYPES[dtype]
+    check_product(y, lo.mx_values(a.double().numpy(), fmt), lo.mx_values(b.double().numpy(), fmt), dtype)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m, n", [(5, 200), (200, 300), (3000, 1500)])
+def test_a_nan_stays_in_its_row_and_column(m, n, fmt):
+    a, b = matrix(m, 320, "f32", 1, 0.5), matrix(n, 320, "f32", 2, 0.5)
+    clean = lm.mx_matmul(lm.mx_quantize(a.cuda(), fmt), lm.mx_quantize(b.cuda(), fmt), torch.float32)
+    a[3, 100], b[n - 2, 319] = float("nan"), float("-inf")
+    y = lm.mx_matmul(lm.mx_quantize(a.cuda(), fmt), lm.mx_quantize(b.cuda(), fmt), torch.float32)
+    bad = torch.zeros(m, n, dtype=torch.bool)
+    bad[3], bad[:, n - 2] = True, True
+    assert torch.equal(y.isnan().cpu(), bad) and torch.equal(y[~bad.cuda()], clean[~bad.cuda()])
+
+
+def test_scales_of_any_size():
+    a, b = torch.ones(3, 64), torch.ones(130, 64)
+    a[0] *= 2.0 ** 100
+    a[1] *= 2.0 ** -100
+    b[0] *= 2.0 ** 20
+    b[1] *= 2.0 ** 60
+    for fmt in FORMATS:
+        y = lm.mx_matmul(lm.mx_quantize(a.cuda(), fmt), lm.mx_quantize(b.cuda(), fmt), torch.float32).cpu()
+        assert torch.equal(y, (a.double() @ b.double().t()).float())
+
+
+def test_out_rows_may_be_apart_and_nothing_else_is_written():
+    a, b = matrix(50, 96, "bf16", 3, 0.5), matrix(90, 96, "bf16", 4, 0.5)
+    qa, qb = lm.mx_quantize(a.cuda(), "e4m3"), lm.mx_quantize(b.cuda(), "e4m3")
+    for m, n, p, q in ((50, 90, qa, qb), (90, 50, qb, qa)):
+        out = torch.full((m + 2, 128), 7.0, device="cuda")
+        binding.div_mx_matmul(p.blob.data_ptr(), p.blob.numel(), q.blob.data_ptr(), q.blob.numel(), m, n, 96, "e4m3", out[1:].data_ptr(), 128, "f32",
+                              binding.current_stream_handle())
+        assert torch.equal(out[1:m + 1, :n], lm.mx_matmul(p, q, torch.float32))
+        assert (out[0] == 7).all() and (out[m + 1] == 7).all() and (out[:, n:] == 7).all()
+
+
+def test_results_repeat_and_survive_a_graph_and_another_stream():
+    a, b = matrix(3, 4096, "bf16", 8, 0.5).cuda(), matrix(500, 4096, "bf16", 9, 0.5).cuda()
+    w = lm.mx_quantize(b, "e2m1")
+    want = lm.mx_matmul(lm.mx_quantize(a, "e2m1"), w)
+    for _ in range(5):
+        assert torch.equal(lm.mx_matmul(lm.mx_quantize(a, "e2m1"), w), want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = lm.mx_matmul(lm.mx_quantize(a, "e2m1"), w)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = lm.mx_matmul(lm.mx_quantize(a, "e2m1"), w)
+    a.mul_(2)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want * 2)
+
+
+def test_a_long_matrix_passes_32_bits():
+    rows, cols = 70000, 65536                                   # 4.6e9 numbers
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[rows - 1, cols - 64:] = torch.arange(64, device="cuda")
+    x[rows - 300, :32] = 3.0
+    q = lm.mx_quantize(x, "e2m1")
+    del x
+    y = q.dequantize(torch.bfloat16)
+    assert float(y[rows - 300, :32].float().sum()) == 96.0
+    same(y[rows - 1:, cols - 64:], lo.mx_values(np.arange(64.0)[None], "e2m1"))
+    assert int(torch.count_nonzero(y[:rows - 300])) == 0
+    one = lm.mx_quantize(torch.ones(1, cols, device="cuda"), "e2m1")
+    p = lm.mx_matmul(q, one, torch.float32)
+    assert float(p[rows - 1, 0]) == lo.mx_values(np.arange(64.0)[None], "e2m1").sum() and float(p[rows - 300, 0]) == 96.0
+    assert int(torch.count_nonzero(p)) == 2
