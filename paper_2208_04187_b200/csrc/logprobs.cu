@@ -6,18 +6,21 @@
 // m and log s are kept apart: their sum would lose log s next to a large m.
 //
 // Forward is bound by memory where the vocabulary is long (one reading of the logits), by the exponentials next (16 a clock and SM).  A
-// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, and joins its sums with the others' in a
-// fixed order.
+// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, LP_AT_ONCE of them under way together, and
+// joins its sums with the others' in a fixed order.  Additions and products go two at a time (f32x2).
 //
-// The most probable tokens come from the same pass: the k-th largest of the CTA's threads' maxima is a bound that at least k logits
-// reach, so that only threads whose maximum reaches it (about k of them) have their pieces read again, out of L2, by whole warps.  What passes
-// the bound goes into a sorted list across a warp's lanes; the warps' lists, and the cluster's, are joined by counting ranks.
+// The most probable tokens come from the same pass.  The k-th largest of the 64 maxima of the CTA's groups of 4 threads is a bound that
+// at least k logits reach; few others do (k-th of 64 groups: the N best logits lie in about 64 (1 - exp(-N/64)) groups, so that 20 groups
+// are reached by 24).  Threads whose own maximum reaches it have their pieces read again, out of L2, by whole warps, and what
+// reaches the bound is collected and ranked by counting.  Where more than LP_THREADS logits reach it (many equal ones, sorted rows,
+// NaN) each warp keeps a sorted list across its lanes instead, and the lists are ranked.
 #include "mx.cuh"
 
 namespace divk {
 
 constexpr uint32_t LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_MAX_TOP = 32, LP_MAX_CLUSTER = 8;
 constexpr float LP_LOG2E = 1.4426950408889634f;
+constexpr uint32_t LP_AT_ONCE = 8;              // pieces of a thread under way
 constexpr float LP_LEAST = -1000.f;             // exp of it is 0, and 0 times it is no NaN
 
 struct LogprobParams {
@@ -62,22 +65,103 @@ __device__ __forceinline__ Running join(Running a, const Running& b) {
     a.t += c.t;
     return a;
 }
-// a number of the row: r.m is at least x
-__device__ __forceinline__ void take(Running& r, float base, float x) {
-    const float a = max_nan(x - base, LP_LEAST), e = exp2_fast(a * LP_LOG2E);
-    r.s += e;
-    r.t = fmaf(e, a, r.t);
+// two numbers in one register pair
+__device__ __forceinline__ uint64_t two(float a, float b) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
 }
-template <int N>
-__device__ __forceinline__ void take_all(Running& r, const float (&v)[N]) {
-    float m = v[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
-    rescale(r, m);
-    const float base = r.m == -INFINITY ? 0.f : r.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) take(r, base, v[i]);
+__device__ __forceinline__ void one_each(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
 }
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+    uint64_t v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+// a thread's sums, in two halves
+struct Sums {
+    float m;
+    uint64_t s, t;
+    __device__ __forceinline__ void raise(float to) {
+        if (to > m) {
+            if (m != -INFINITY) {
+                const float d = max_nan(m - to, LP_LEAST), c = exp2_fast(d * LP_LOG2E);
+                t = mul_two(two(c, c), fma_two(s, two(d, d), t));
+                s = mul_two(two(c, c), s);
+            }
+            m = to;
+        }
+    }
+    // two numbers, neither above m (base: m, or 0 where nothing but -inf has come yet)
+    __device__ __forceinline__ void take(uint64_t x, uint64_t minus_base) {
+        float a, b;
+        one_each(add_two(x, minus_base), a, b);
+        a = max_nan(a, LP_LEAST);
+        b = max_nan(b, LP_LEAST);
+        const uint64_t ab = two(a, b);
+        one_each(mul_two(ab, two(LP_LOG2E, LP_LOG2E)), a, b);
+        const uint64_t e = two(exp2_fast(a), exp2_fast(b));
+        s = add_two(s, e);
+        t = fma_two(e, ab, t);
+    }
+    __device__ __forceinline__ Running whole() const {
+        Running r;
+        float s1, t1;
+        r.m = m;
+        one_each(s, r.s, s1);
+        one_each(t, r.t, t1);
+        r.s += s1;
+        r.t += t1;
+        return r;
+    }
+};
+// 16 bytes of the row: their largest, and their pairs in 32 bits
+template <typename T> struct Quad;
+template <> struct Quad<float> {
+    static __device__ __forceinline__ float largest(const uint4& q) {
+        return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+    }
+    static __device__ __forceinline__ void take(Sums& r, const uint4& q, uint64_t minus_base) {
+        r.take(two(__uint_as_float(q.x), __uint_as_float(q.y)), minus_base);
+        r.take(two(__uint_as_float(q.z), __uint_as_float(q.w)), minus_base);
+    }
+};
+template <> struct Quad<__nv_bfloat16> {
+    static __device__ __forceinline__ float largest(const uint4& q) {
+        const __nv_bfloat162 *a = reinterpret_cast<const __nv_bfloat162*>(&q);
+        const __nv_bfloat162 m = __hmax2(__hmax2(a[0], a[1]), __hmax2(a[2], a[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ void take(Sums& r, const uint4& q, uint64_t minus_base) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.take(two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)), minus_base);
+    }
+};
+template <> struct Quad<__half> {
+    static __device__ __forceinline__ float largest(const uint4& q) {
+        const __half2* a = reinterpret_cast<const __half2*>(&q);
+        const __half2 m = __hmax2(__hmax2(a[0], a[1]), __hmax2(a[2], a[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ void take(Sums& r, const uint4& q, uint64_t minus_base) {
+        const __half2* a = reinterpret_cast<const __half2*>(&q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(a[i]);
+            r.take(two(f.x, f.y), minus_base);
+        }
+    }
+};
 
 // ---------------------------------------------------------------------------------------------
 // 16-byte pieces of a row that may begin anywhere: piece 0 ends at the first multiple of 16 bytes
@@ -155,13 +239,14 @@ struct TopList {            // across the lanes of a warp, best first
     }
 };
 
+constexpr uint32_t LP_GROUPS = LP_THREADS / 4;
 struct LogprobShared {
+    alignas(16) uint32_t maxima[LP_GROUPS];         // keys of the groups' maxima
     Running warps[LP_WARPS];
     Running cta;
-    alignas(16) uint32_t maxima[LP_THREADS];        // keys of the threads' maxima
-    uint32_t bound, n_again;
+    uint32_t bound, n_again, n_found;
     uint32_t again[LP_THREADS];                     // threads whose pieces are read again
-    uint32_t key[LP_THREADS], index[LP_THREADS];     // the warps' lists, then (of rank 0) the cluster's
+    uint32_t key[LP_THREADS], index[LP_THREADS];     // what reaches the bound; the warps' lists; (of rank 0) the cluster's
     uint32_t best_key[LP_MAX_TOP], best_index[LP_MAX_TOP];
 };
 static_assert(LP_WARPS * LP_MAX_TOP == LP_THREADS && LP_MAX_CLUSTER * LP_MAX_TOP <= LP_THREADS, "a list entry for each thread");
@@ -177,12 +262,12 @@ __device__ __forceinline__ uint32_t lp_peer(uint32_t local, uint32_t rank) {
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
-// the `top` best of the entries in sh.key, sh.index go to sh.best_key, sh.best_index (key 0: no entry); all threads together
-__device__ __forceinline__ void lp_rank_entries(LogprobShared& sh, uint32_t top) {
-    const uint32_t k = sh.key[threadIdx.x], i = sh.index[threadIdx.x];
-    if (k != 0u) {
+// the `top` best of the first n entries in sh.key, sh.index go to sh.best_key, sh.best_index (key 0: no entry); all threads together
+__device__ __forceinline__ void lp_rank_entries(LogprobShared& sh, uint32_t n, uint32_t top) {
+    if (threadIdx.x < n && sh.key[threadIdx.x] != 0u) {
+        const uint32_t k = sh.key[threadIdx.x], i = sh.index[threadIdx.x];
         uint32_t better = 0;
-        for (uint32_t j = 0; j < LP_THREADS; ++j) better += before(sh.key[j], sh.index[j], k, i) ? 1u : 0u;
+        for (uint32_t j = 0; j < n; ++j) better += before(sh.key[j], sh.index[j], k, i) ? 1u : 0u;
         if (better < top) {
             sh.best_key[better] = k;
             sh.best_index[better] = i;
@@ -202,21 +287,55 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
     const P pieces(static_cast<const XT*>(p.x) + row * p.stride, p.vocab);
     const uint32_t from = (uint32_t)((uint64_t)pieces.count * rank / p.split), to = (uint32_t)((uint64_t)pieces.count * (rank + 1u) / p.split);
 
-    Running r = {-INFINITY, 0.f, 0.f};
-    constexpr uint32_t AT_ONCE = 4;
+    Sums sums = {-INFINITY, 0ull, 0ull};
+    // whole pieces: all but perhaps the row's first and its last
+    const uint32_t w0 = max(from, pieces.first ? 1u : 0u), w1 = min(to, pieces.count - (pieces.size(pieces.count - 1u) < P::N ? 1u : 0u));
+    const uint4* quads = reinterpret_cast<const uint4*>(pieces.row + pieces.first) - (pieces.first ? 1 : 0);       // (piece 0 is not read there)
     uint32_t piece = from + threadIdx.x;
-    for (; piece + (AT_ONCE - 1u) * LP_THREADS < to; piece += AT_ONCE * LP_THREADS) {
-        float v[AT_ONCE][P::N];
+    if (piece < w0) piece += LP_THREADS;
+    for (; piece + (LP_AT_ONCE - 1u) * LP_THREADS < w1; piece += LP_AT_ONCE * LP_THREADS) {
+        uint4 q[LP_AT_ONCE];
 #pragma unroll
-        for (uint32_t u = 0; u < AT_ONCE; ++u) pieces.get(piece + u * LP_THREADS, v[u]);
+        for (uint32_t u = 0; u < LP_AT_ONCE; ++u) q[u] = quads[piece + u * LP_THREADS];
+        float m = Quad<XT>::largest(q[0]);
 #pragma unroll
-        for (uint32_t u = 0; u < AT_ONCE; ++u) take_all(r, v[u]);
+        for (uint32_t u = 1; u < LP_AT_ONCE; ++u) m = fmaxf(m, Quad<XT>::largest(q[u]));
+        sums.raise(m);
+        const float base = sums.m == -INFINITY ? 0.f : sums.m;
+        const uint64_t minus = two(-base, -base);
+#pragma unroll
+        for (uint32_t u = 0; u < LP_AT_ONCE; ++u) Quad<XT>::take(sums, q[u], minus);
     }
-    for (; piece < to; piece += LP_THREADS) {
-        float v[P::N];
-        pieces.get(piece, v);
-        take_all(r, v);
+    {
+        // the rest, still all under way together
+        uint4 q[LP_AT_ONCE];
+#pragma unroll
+        for (uint32_t u = 0; u < LP_AT_ONCE; ++u)
+            if (piece + u * LP_THREADS < w1) q[u] = quads[piece + u * LP_THREADS];
+#pragma unroll
+        for (uint32_t u = 0; u < LP_AT_ONCE; ++u) {
+            if (piece + u * LP_THREADS < w1) {
+                sums.raise(Quad<XT>::largest(q[u]));
+                const float base = sums.m == -INFINITY ? 0.f : sums.m;
+                Quad<XT>::take(sums, q[u], two(-base, -base));
+            }
+        }
     }
+    // the first and the last piece, if cut: by the thread whose they are
+    for (uint32_t end = 0; end < 2u; ++end) {
+        const uint32_t cut = end ? pieces.count - 1u : 0u;
+        if (cut >= from && cut < to && (cut < w0 || cut >= w1) && (end == 0u || cut != 0u) && (cut - from) % LP_THREADS == threadIdx.x) {
+            float v[P::N];
+            pieces.get(cut, v);
+#pragma unroll
+            for (uint32_t i = 0; i < P::N; i += 2u) {
+                sums.raise(fmaxf(v[i], v[i + 1u]));
+                const float base = sums.m == -INFINITY ? 0.f : sums.m;
+                sums.take(two(v[i], v[i + 1u]), two(-base, -base));
+            }
+        }
+    }
+    Running r = sums.whole();
     const float thread_max = r.m;
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
@@ -229,9 +348,11 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
         r = join(low ? r : o, low ? o : r);
     }
     if (lane == 0) sh.warps[warp] = r;
+    const uint32_t mine = TOP && from + threadIdx.x < to ? order_key(thread_max) : 0u;
     if (TOP) {
-        sh.maxima[threadIdx.x] = from + threadIdx.x < to ? order_key(thread_max) : 0u;
-        if (threadIdx.x == 0) sh.n_again = 0;
+        const uint32_t pair = max(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, 1)), group = max(pair, __shfl_xor_sync(0xFFFFFFFFu, pair, 2));
+        if ((lane & 3u) == 0) sh.maxima[threadIdx.x >> 2] = group;
+        if (threadIdx.x == 0) sh.n_again = sh.n_found = 0;
     }
     __syncthreads();
     r = sh.warps[0];
@@ -239,45 +360,75 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
     if (threadIdx.x == 0) sh.cta = r;
 
     if (TOP) {
-        // the top-th largest of the threads' maxima; 0 (everything) where not that many threads had a piece.  A sum that is NaN may come
-        // from a NaN, which no maximum shows: everything is read again.
-        const uint32_t mine = sh.maxima[threadIdx.x];
+        // the top-th largest of the groups' maxima; 0 (everything) where not that many groups had a piece.  A sum that is NaN may come
+        // from a NaN, which no maximum shows: everything is read again.  (4 threads count for a group, a quarter of the others each.)
+        const uint32_t group = sh.maxima[threadIdx.x >> 2];
         uint32_t above = 0, reach = 0;
-        for (uint32_t j = 0; j < LP_THREADS; j += 4) {
-            const uint4 k = *reinterpret_cast<const uint4*>(&sh.maxima[j]);
-            above += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
-            reach += (k.x >= mine) + (k.y >= mine) + (k.z >= mine) + (k.w >= mine);
-        }
-        if (above < p.top && reach >= p.top) sh.bound = mine;       // (all that write, write the same)
-        __syncthreads();
-        const uint32_t bound = r.s != r.s ? 0u : sh.bound;
-        if (from + threadIdx.x < to && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1u)] = threadIdx.x;
-        __syncthreads();
-        TopList list = {0u, 0xFFFFFFFFu};
-        uint32_t last_key = 0u, last_index = 0xFFFFFFFFu;
-        const uint32_t each = (to - from + LP_THREADS - 1u) / LP_THREADS;          // pieces of a thread, at most
-        const uint32_t runs = (each + 31u) / 32u, jobs = sh.n_again * runs;
-        for (uint32_t job = warp; job < jobs; job += LP_WARPS) {
-            const uint32_t at = from + sh.again[job / runs] + (job % runs * 32u + lane) * LP_THREADS;
-            float v[P::N];
 #pragma unroll
-            for (uint32_t i = 0; i < P::N; ++i) v[i] = -INFINITY;
-            const uint32_t n = at < to ? pieces.size(at) : 0u, first = at < to ? pieces.begin(at) : 0u;
-            if (n) pieces.get(at, v);
-#pragma unroll
-            for (uint32_t i = 0; i < P::N; ++i) {
-                const uint32_t k = order_key(v[i]);
-                list.offer(i < n && k >= bound, k, first + i, p.top, last_key, last_index);
-            }
+        for (uint32_t j = 0; j < LP_GROUPS / 4u; j += 4u) {
+            const uint4 k = *reinterpret_cast<const uint4*>(&sh.maxima[(lane & 3u) * (LP_GROUPS / 4u) + j]);
+            above += (k.x > group) + (k.y > group) + (k.z > group) + (k.w > group);
+            reach += (k.x >= group) + (k.y >= group) + (k.z >= group) + (k.w >= group);
         }
-        sh.key[threadIdx.x] = lane < p.top ? list.key : 0u;
-        sh.index[threadIdx.x] = lane < p.top ? list.index : 0xFFFFFFFFu;
+        uint32_t both = above << 16 | reach;
+        both += __shfl_xor_sync(0xFFFFFFFFu, both, 1);
+        both += __shfl_xor_sync(0xFFFFFFFFu, both, 2);
+        if ((both >> 16) < p.top && (both & 0xFFFFu) >= p.top) sh.bound = group;       // (all that write, write the same)
         if (threadIdx.x < LP_MAX_TOP) {                    // (a CTA of a cluster may hold fewer than `top`)
             sh.best_key[threadIdx.x] = 0u;
             sh.best_index[threadIdx.x] = 0xFFFFFFFFu;
         }
         __syncthreads();
-        lp_rank_entries(sh, p.top);
+        const uint32_t bound = r.s != r.s ? 0u : sh.bound;
+        if (from + threadIdx.x < to && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1u)] = threadIdx.x;
+        __syncthreads();
+        const uint32_t each = (to - from + LP_THREADS - 1u) / LP_THREADS;          // pieces of a thread, at most
+        const uint32_t runs = (each + 31u) / 32u, jobs = sh.n_again * runs;
+        for (uint32_t job = warp; job < jobs; job += LP_WARPS) {
+            const uint32_t at = from + sh.again[job / runs] + (job % runs * 32u + lane) * LP_THREADS;
+            if (*(volatile uint32_t*)&sh.n_found > LP_THREADS) break;                // (lists are the way then)
+            if (at < to) {
+                float v[P::N];
+                pieces.get(at, v);
+                const uint32_t n = pieces.size(at), first = pieces.begin(at);
+#pragma unroll
+                for (uint32_t i = 0; i < P::N; ++i) {
+                    const uint32_t k = order_key(v[i]);
+                    if (i < n && k >= bound) {
+                        const uint32_t slot = atomicAdd(&sh.n_found, 1u);
+                        if (slot < LP_THREADS) {
+                            sh.key[slot] = k;
+                            sh.index[slot] = first + i;
+                        }
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        uint32_t n = sh.n_found;
+        if (n > LP_THREADS) {
+            __syncthreads();                               // (nobody writes entries before all have seen the count)
+            TopList list = {0u, 0xFFFFFFFFu};
+            uint32_t last_key = 0u, last_index = 0xFFFFFFFFu;
+            for (uint32_t job = warp; job < jobs; job += LP_WARPS) {
+                const uint32_t at = from + sh.again[job / runs] + (job % runs * 32u + lane) * LP_THREADS;
+                float v[P::N];
+#pragma unroll
+                for (uint32_t i = 0; i < P::N; ++i) v[i] = -INFINITY;
+                const uint32_t have = at < to ? pieces.size(at) : 0u, first = at < to ? pieces.begin(at) : 0u;
+                if (have) pieces.get(at, v);
+#pragma unroll
+                for (uint32_t i = 0; i < P::N; ++i) {
+                    const uint32_t k = order_key(v[i]);
+                    list.offer(i < have && k >= bound, k, first + i, p.top, last_key, last_index);
+                }
+            }
+            sh.key[threadIdx.x] = lane < p.top ? list.key : 0u;
+            sh.index[threadIdx.x] = lane < p.top ? list.index : 0xFFFFFFFFu;
+            n = LP_THREADS;
+            __syncthreads();
+        }
+        lp_rank_entries(sh, n, p.top);
     }
     if (p.split > 1u) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -301,7 +452,7 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
                 sh.key[threadIdx.x] = k;
                 sh.index[threadIdx.x] = i;
                 __syncthreads();
-                lp_rank_entries(sh, p.top);
+                lp_rank_entries(sh, LP_THREADS, p.top);
             }
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -337,6 +488,45 @@ struct LogprobBackParams {
 };
 constexpr uint32_t LP_BACK_EACH = 4;          // pieces of a thread
 
+// pairs of dlogits -> 16 bytes
+template <typename T> struct Pack;
+template <> struct Pack<float> {
+    static __device__ __forceinline__ void put(uint4& q, int pair, float a, float b) {
+        if (pair == 0) q.x = __float_as_uint(a), q.y = __float_as_uint(b);
+        else q.z = __float_as_uint(a), q.w = __float_as_uint(b);
+    }
+    static __device__ __forceinline__ uint64_t get(const uint4& q, int pair) {
+        return pair == 0 ? two(__uint_as_float(q.x), __uint_as_float(q.y)) : two(__uint_as_float(q.z), __uint_as_float(q.w));
+    }
+};
+template <> struct Pack<__nv_bfloat16> {
+    static __device__ __forceinline__ void put(uint4& q, int pair, float a, float b) { reinterpret_cast<__nv_bfloat162*>(&q)[pair] = __floats2bfloat162_rn(a, b); }
+    static __device__ __forceinline__ uint64_t get(const uint4& q, int pair) {
+        const uint32_t w = reinterpret_cast<const uint32_t*>(&q)[pair];
+        return two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+};
+template <> struct Pack<__half> {
+    static __device__ __forceinline__ void put(uint4& q, int pair, float a, float b) { reinterpret_cast<__half2*>(&q)[pair] = __floats2half2_rn(a, b); }
+    static __device__ __forceinline__ uint64_t get(const uint4& q, int pair) {
+        const float2 f = __half22float2(reinterpret_cast<const __half2*>(&q)[pair]);
+        return two(f.x, f.y);
+    }
+};
+struct Slope {                                // of a row
+    float m, log_s, dent, c0, dlp;
+    // -p (dent log p + c0) of two logits
+    __device__ __forceinline__ void apply(uint64_t x, float& a, float& b) const {
+        one_each(add_two(add_two(x, two(-m, -m)), two(-log_s, -log_s)), a, b);
+        const uint64_t lp = two(max_nan(a, LP_LEAST), max_nan(b, LP_LEAST));
+        one_each(mul_two(lp, two(LP_LOG2E, LP_LOG2E)), a, b);
+        const uint64_t p = two(-exp2_fast(a), -exp2_fast(b));
+        one_each(mul_two(p, fma_two(two(dent, dent), lp, two(c0, c0))), a, b);
+    }
+};
+
+// A thread takes LP_BACK_EACH pieces, their reads under way together; the target's number is stored once more by the thread whose it is.
+// Bound by memory: one reading, one writing.
 template <typename XT>
 __global__ void __launch_bounds__(LP_THREADS)
 logprob_backward_kernel(const __grid_constant__ LogprobBackParams p) {
@@ -347,47 +537,59 @@ logprob_backward_kernel(const __grid_constant__ LogprobBackParams p) {
     const P pieces(static_cast<const XT*>(p.x) + row * p.stride, p.vocab);
     XT* out = static_cast<XT*>(p.dx) + (uint64_t)row * p.vocab;
     const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(pieces.row)) & 15u) == 0;      // pieces begin alike
-    float v[LP_BACK_EACH][P::N];
-    const uint32_t first = chunk * LP_THREADS * LP_BACK_EACH + threadIdx.x;
+    const uint32_t c0 = chunk * LP_THREADS * LP_BACK_EACH, first = c0 + threadIdx.x;
+    // all pieces of the CTA are whole ones, and written as they are read
+    const bool plain = same && c0 + LP_THREADS * LP_BACK_EACH < pieces.count && (c0 != 0u || pieces.first == 0u);
+    uint4 q[LP_BACK_EACH];
+    if (plain) {
 #pragma unroll
-    for (uint32_t u = 0; u < LP_BACK_EACH; ++u)
-        if (first + u * LP_THREADS < pieces.count) pieces.get(first + u * LP_THREADS, v[u]);
-    const float m = p.stats[2ull * row], log_s = p.stats[2ull * row + 1u];
+        for (uint32_t u = 0; u < LP_BACK_EACH; ++u) q[u] = __ldcs(reinterpret_cast<const uint4*>(pieces.row + pieces.begin(first + u * LP_THREADS)));
+    }
+    Slope s;
+    s.m = p.stats[2ull * row];
+    s.log_s = p.stats[2ull * row + 1u];
     const int64_t target = p.targets[row];
-    float dlp = p.dlogprobs ? p.dlogprobs[row] : 0.f;
-    if (target < 0 || log_s == INFINITY) dlp = 0.f;
-    else if (target >= (int64_t)p.vocab) dlp = __uint_as_float(0x7FC00000u);
-    const float dent = p.dentropy ? p.dentropy[row] : 0.f;
-    const float c0 = p.dentropy ? fmaf(dent, p.entropy[row], dlp) : dlp;
+    s.dlp = p.dlogprobs ? p.dlogprobs[row] : 0.f;
+    if (target < 0 || s.log_s == INFINITY) s.dlp = 0.f;
+    else if (target >= (int64_t)p.vocab) s.dlp = __uint_as_float(0x7FC00000u);
+    s.dent = p.dentropy ? p.dentropy[row] : 0.f;
+    s.c0 = p.dentropy ? fmaf(s.dent, p.entropy[row], s.dlp) : s.dlp;
     const uint32_t hit = target >= 0 && target < (int64_t)p.vocab ? (uint32_t)target : 0xFFFFFFFFu;
+    if (plain) {
 #pragma unroll
-    for (uint32_t u = 0; u < LP_BACK_EACH; ++u) {
-        const uint32_t piece = first + u * LP_THREADS;
-        if (piece >= pieces.count) continue;
-        const uint32_t begin = pieces.begin(piece), n = pieces.size(piece);
+        for (uint32_t u = 0; u < LP_BACK_EACH; ++u) {
+            const uint32_t begin = pieces.begin(first + u * LP_THREADS);
+            uint4 d;
 #pragma unroll
-        for (uint32_t i = 0; i < P::N; ++i) {
-            const float lp = max_nan((v[u][i] - m) - log_s, LP_LEAST), e = exp2_fast(lp * LP_LOG2E);
-            const float d = -e * fmaf(dent, lp, c0);
-            v[u][i] = begin + i == hit ? d + dlp : d;
-        }
-        if (n == P::N && same) {
-            uint32_t w[4];
-            if (sizeof(XT) == 4) {
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) w[i] = __float_as_uint(v[u][i]);
-            } else {
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const XT a = from_f32<XT>(v[u][(2 * i) % P::N]), b = from_f32<XT>(v[u][(2 * i + 1) % P::N]);
-                    w[i] = *reinterpret_cast<const unsigned short*>(&a) | (uint32_t)*reinterpret_cast<const unsigned short*>(&b) << 16;
-                }
+            for (int i = 0; i < (int)P::N / 2; ++i) {
+                float a, b;
+                s.apply(Pack<XT>::get(q[u], i), a, b);
+                Pack<XT>::put(d, i, a, b);
             }
-            *reinterpret_cast<uint4*>(out + begin) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
+            __stcs(reinterpret_cast<uint4*>(out + begin), d);
+        }
+    } else {
+        for (uint32_t u = 0; u < LP_BACK_EACH; ++u) {
+            const uint32_t piece = first + u * LP_THREADS;
+            if (piece >= pieces.count) break;
+            const uint32_t begin = pieces.begin(piece), n = pieces.size(piece);
+            float v[P::N];
+            pieces.get(piece, v);
 #pragma unroll
-            for (uint32_t i = 0; i < P::N; ++i)
-                if (i < n) out[begin + i] = from_f32<XT>(v[u][i]);
+            for (uint32_t i = 0; i < P::N; i += 2u) {
+                float a, b;
+                s.apply(two(v[i], v[i + 1u]), a, b);
+                if (i < n) out[begin + i] = from_f32<XT>(a);
+                if (i + 1u < n) out[begin + i + 1u] = from_f32<XT>(b);
+            }
+        }
+    }
+    if (hit != 0xFFFFFFFFu) {
+        const uint32_t piece = pieces.first ? (hit < pieces.first ? 0u : 1u + (hit - pieces.first) / P::N) : hit / P::N;
+        if (piece >= c0 && piece - c0 < LP_THREADS * LP_BACK_EACH && (piece - c0) % LP_THREADS == threadIdx.x) {
+            float a, b;
+            s.apply(two(to_f32(pieces.row[hit]), 0.f), a, b);
+            out[hit] = from_f32<XT>(a + s.dlp);
         }
     }
 }
