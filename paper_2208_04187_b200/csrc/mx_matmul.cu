@@ -5,11 +5,11 @@
 // One of the operands, P, fills the 128 lanes of the accumulator, the other, S, its BN columns.  S is the operand with fewer
 // rows where those fit one tile (few tokens: the weights then fill the lanes, and the tile is as narrow as the tokens), else B.
 //
-// A CTA makes one tile of 128 x BN.  A producer thread brings stages of 128 bytes of each row, codes and scales, into a ring with
-// plain bulk copies: tiles lie in the blobs as the instruction wants them.  The issuer thread waits for a stage, has its scales
-// copied into tensor memory, issues the stage's 4 products of 32 bytes of each row, and commits; the commit hands the stage back.  The
-// columns of scales go round with the ring, so that no copy meets a product that still reads them.  Four warps then bring
-// the tile from tensor memory to the output.
+// A CTA makes tiles of 128 x BN, one after another.  A producer thread brings stages of 128 bytes of each row, codes and scales, into a
+// ring with plain bulk copies: tiles lie in the blobs as the instruction wants them.  The issuer thread waits for a stage, has its
+// scales copied into tensor memory, issues the stage's 4 products of 32 bytes of each row, and commits; the commit hands the stage
+// back.  The columns of scales go round with the ring, so that no copy meets a product that still reads them.  Eight warps bring a tile
+// from tensor memory to registers, give the accumulator back, and store while the next tile is on its way.
 //
 // Where there are fewer tiles than SMs, the sum over k is split among the CTAs of a cluster: each sums a run of stages, leaves its tile
 // in its shared memory, and takes a share of the columns, which it adds up over the cluster in the order of the ranks (the result
@@ -21,8 +21,8 @@
 
 namespace divk {
 
-constexpr uint32_t MXP_THREADS = 192;             // 4 warps for the way out, the producer's, the issuer's
-constexpr uint32_t MXP_MAX_STAGES = 8;
+constexpr uint32_t MXP_OUT_WARPS = 8, MXP_PRODUCER = 8, MXP_ISSUER = 9, MXP_THREADS = 320;
+constexpr uint32_t MXP_MAX_STAGES = 8, MXP_SMS = 148;
 constexpr uint64_t MXP_LIMIT_NS = 2000000000ull;
 constexpr uint32_t MXP_SMEM = 224u * 1024u;       // of a CTA, ring and control block
 
@@ -34,14 +34,14 @@ struct MxProductParams {
     MxSide p, s;
     void* out;
     uint64_t ld;                 // numbers between two rows of out
-    uint32_t tiles_p;
+    uint32_t tiles_p, tiles;
     uint32_t swapped;            // the lanes are columns of out
     uint32_t out_dtype;
     uint32_t split;              // CTAs of a cluster
     uint32_t vec;                // out: 16-byte stores along a row
 };
 struct MxCtl {
-    uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES], done;
+    uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES], done, taken;      // done: a tile is summed; taken: it is in registers
     uint32_t tmem, failed;
 };
 
@@ -55,6 +55,8 @@ template <int FMT, uint32_t BN> struct MxTile {
     static constexpr uint32_t SCALE_COLUMNS = 4u * F::ATOMS * (1u + S_BLOCKS);
     static constexpr uint32_t STAGES = FIT < MXP_MAX_STAGES ? FIT : MXP_MAX_STAGES;
     static constexpr uint32_t SMEM = 1024u + STAGES * STAGE_BYTES + (uint32_t)sizeof(MxCtl);
+    static constexpr uint32_t HALVES = BN >= 64u ? 2u : 1u;                   // warps 4..7 take the upper columns of wide tiles
+    static constexpr uint32_t MINE = BN / HALVES;                             // columns of a warp
     static constexpr uint32_t NEEDED = BN + SCALE_COLUMNS * STAGES;
     static constexpr uint32_t COLUMNS = NEEDED <= 128u ? 128u : NEEDED <= 256u ? 256u : 512u;
     static_assert(NEEDED <= 512u && STAGES >= 2u, "tensor memory");
@@ -183,13 +185,11 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
     MxCtl* ctl = reinterpret_cast<MxCtl*>(ring + T::STAGES * T::STAGE_BYTES);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
 
-    const uint32_t rank = p.split > 1u ? cluster_rank() : 0u, tile = blockIdx.x / p.split;
-    const uint32_t tp = tile % p.tiles_p, ts = tile / p.tiles_p;
+    const uint32_t rank = p.split > 1u ? cluster_rank() : 0u, first = blockIdx.x / p.split, step = gridDim.x / p.split;
     const uint32_t all = p.p.s.stages;
     const uint32_t k0 = (uint32_t)((uint64_t)all * rank / p.split), k1 = (uint32_t)((uint64_t)all * (rank + 1u) / p.split);
-    const uint32_t p0 = tp * 128u, s0 = ts * BN;
 
-    if (warp == 5) {
+    if (warp == MXP_ISSUER) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem)), "n"(T::COLUMNS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -199,6 +199,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             mbar_init(&ctl->empty[i], 1);
         }
         mbar_init(&ctl->done, 1);
+        mbar_init(&ctl->taken, 4u * T::HALVES);
         ctl->failed = 0;
         fence_barrier_init();
         fence_proxy_async();
@@ -210,127 +211,137 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
     griddep_wait();
     griddep_launch();
 
-    if (warp == 4 && lane == 0) {
-        // ---- producer ----
-        const uint32_t hp = mx_tile_rows(p.p.s, tp) * 128u;
-        // rows of S: of its only block of 128 (BN < 128), or BN / 128 whole blocks
-        uint32_t hs[T::S_BLOCKS];
-        const unsigned char* from_s[T::S_BLOCKS];
-        const unsigned char* scales_s[T::S_BLOCKS];
-        uint32_t step_s[T::S_BLOCKS];
-        uint32_t bytes = hp + T::SCALES;
-#pragma unroll
-        for (uint32_t b = 0; b < T::S_BLOCKS; ++b) {
-            const uint32_t row = s0 + b * 128u, rb = row / 128u;
-            const bool there = row < p.s.s.rows;
-            const uint32_t height = there ? mx_tile_rows(p.s.s, rb) : 0u;
-            hs[b] = min(height, BN) * 128u;
-            from_s[b] = p.s.codes + (there ? mx_tile_offset(p.s.s, rb, 0) : 0u);
-            step_s[b] = height * 128u;
-            scales_s[b] = p.s.scales + (uint64_t)(there ? rb : 0u) * p.s.s.stages * T::SCALES;
-            bytes += hs[b] + T::SCALES;                       // (scales of a block that is not there: those of the first, for columns that nobody keeps)
-        }
-        const unsigned char* from_p = p.p.codes + mx_tile_offset(p.p.s, tp, 0);
-        const unsigned char* scales_p = p.p.scales + (uint64_t)tp * all * T::SCALES;
+    if (warp == MXP_PRODUCER && lane == 0) {
         uint32_t asked = 0;
         bool ok = true;
-        for (uint32_t k = k0; k < k1 && ok; ++k, ++asked) {
-            const uint32_t slot = asked % T::STAGES, turn = asked / T::STAGES;
-            if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl)) {
-                ok = false;
-                break;
-            }
-            unsigned char* at = ring + slot * T::STAGE_BYTES;
-            uint64_t* bar = &ctl->full[slot];
-            mbar_arrive_expect_tx(bar, bytes);
-            bulk_load(at, from_p + (uint64_t)k * hp, hp, bar);
-            bulk_load(at + T::P_CODES + T::S_CODES, scales_p + (uint64_t)k * T::SCALES, T::SCALES, bar);
+        for (uint32_t tile = first; tile < p.tiles && ok; tile += step) {
+            const uint32_t tp = tile % p.tiles_p, s0 = tile / p.tiles_p * BN;
+            const uint32_t hp = mx_tile_rows(p.p.s, tp) * 128u;
+            // rows of S: of its only block of 128 (BN < 128), or BN / 128 whole blocks
+            uint32_t hs[T::S_BLOCKS], step_s[T::S_BLOCKS];
+            const unsigned char *from_s[T::S_BLOCKS], *scales_s[T::S_BLOCKS];
+            uint32_t bytes = hp + T::SCALES;
 #pragma unroll
             for (uint32_t b = 0; b < T::S_BLOCKS; ++b) {
-                if (hs[b]) bulk_load(at + T::P_CODES + b * 16384u, from_s[b] + (uint64_t)k * step_s[b], hs[b], bar);
-                bulk_load(at + T::P_CODES + T::S_CODES + (1u + b) * T::SCALES, scales_s[b] + (uint64_t)k * T::SCALES, T::SCALES, bar);
+                const uint32_t row = s0 + b * 128u, rb = row / 128u;
+                const bool there = row < p.s.s.rows;
+                const uint32_t height = there ? mx_tile_rows(p.s.s, rb) : 0u;
+                hs[b] = min(height, BN) * 128u;
+                from_s[b] = p.s.codes + (there ? mx_tile_offset(p.s.s, rb, 0) : 0u);
+                step_s[b] = height * 128u;
+                scales_s[b] = p.s.scales + (uint64_t)(there ? rb : 0u) * p.s.s.stages * T::SCALES;
+                bytes += hs[b] + T::SCALES;                   // (scales of a block that is not there: those of the first, for columns that nobody keeps)
+            }
+            const unsigned char* from_p = p.p.codes + mx_tile_offset(p.p.s, tp, 0);
+            const unsigned char* scales_p = p.p.scales + (uint64_t)tp * all * T::SCALES;
+            for (uint32_t k = k0; k < k1; ++k, ++asked) {
+                const uint32_t slot = asked % T::STAGES, turn = asked / T::STAGES;
+                if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl)) {
+                    ok = false;
+                    break;
+                }
+                unsigned char* at = ring + slot * T::STAGE_BYTES;
+                uint64_t* bar = &ctl->full[slot];
+                mbar_arrive_expect_tx(bar, bytes);
+                bulk_load(at, from_p + (uint64_t)k * hp, hp, bar);
+                bulk_load(at + T::P_CODES + T::S_CODES, scales_p + (uint64_t)k * T::SCALES, T::SCALES, bar);
+#pragma unroll
+                for (uint32_t b = 0; b < T::S_BLOCKS; ++b) {
+                    if (hs[b]) bulk_load(at + T::P_CODES + b * 16384u, from_s[b] + (uint64_t)k * step_s[b], hs[b], bar);
+                    bulk_load(at + T::P_CODES + T::S_CODES + (1u + b) * T::SCALES, scales_s[b] + (uint64_t)k * T::SCALES, T::SCALES, bar);
+                }
             }
         }
         // no copy may land after the CTA has gone, whoever gave up.  (Slots of earlier fills were handed back full.)
         const uint64_t t0 = now_ns();
         for (uint32_t i = asked > T::STAGES ? asked - T::STAGES : 0u; i < asked; ++i)
             while (!mbar_try_wait(&ctl->full[i % T::STAGES], (i / T::STAGES) & 1u) && now_ns() - t0 < MXP_LIMIT_NS) {}
-    } else if (warp == 5 && lane == 0) {
-        // ---- issuer ----
+    } else if (warp == MXP_ISSUER && lane == 0) {
         // dense, both operands of one type, scales with 8 bits of exponent, BN columns, 128 lanes
         const uint32_t type = FMT == MX_E2M1 ? 1u : 0u;
         const uint32_t idesc0 = type << 7 | type << 10 | (BN >> 3) << 17 | 1u << 23 | (128u >> 4) << 24;
         const uint32_t scales0 = tmem + BN;
+        uint32_t n = 0, made = 0;
         bool ok = true;
-        for (uint32_t k = k0, n = 0; k < k1; ++k, ++n) {
-            const uint32_t slot = n % T::STAGES;
-            if (!mxp_wait(&ctl->full[slot], (n / T::STAGES) & 1u, ctl)) {
+        for (uint32_t tile = first; tile < p.tiles && ok; tile += step, ++made) {
+            if (made > 0u && !mxp_wait(&ctl->taken, (made - 1u) & 1u, ctl)) {
                 ok = false;
                 break;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t at = smem_u32(ring + slot * T::STAGE_BYTES), sc = at + T::P_CODES + T::S_CODES;
-            const uint32_t cp = scales0 + slot * T::SCALE_COLUMNS, cs = cp + 4u * F::ATOMS;
+            for (uint32_t k = k0; k < k1; ++k, ++n) {
+                const uint32_t slot = n % T::STAGES;
+                if (!mxp_wait(&ctl->full[slot], (n / T::STAGES) & 1u, ctl)) {
+                    ok = false;
+                    break;
+                }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = smem_u32(ring + slot * T::STAGE_BYTES), sc = at + T::P_CODES + T::S_CODES;
+                const uint32_t cp = scales0 + slot * T::SCALE_COLUMNS, cs = cp + 4u * F::ATOMS;
 #pragma unroll
-            for (uint32_t a = 0; a < F::ATOMS; ++a) {
-                mxp_scales(cp + 4u * a, mxp_desc(sc + 512u * a, 128u, 0));
+                for (uint32_t a = 0; a < F::ATOMS; ++a) {
+                    mxp_scales(cp + 4u * a, mxp_desc(sc + 512u * a, 128u, 0));
 #pragma unroll
-                for (uint32_t b = 0; b < T::S_BLOCKS; ++b)
-                    mxp_scales(cs + 4u * (a * T::S_BLOCKS + b), mxp_desc(sc + (1u + b) * T::SCALES + 512u * a, 128u, 0));
+                    for (uint32_t b = 0; b < T::S_BLOCKS; ++b)
+                        mxp_scales(cs + 4u * (a * T::S_BLOCKS + b), mxp_desc(sc + (1u + b) * T::SCALES + 512u * a, 128u, 0));
+                }
+                const uint64_t dp = mxp_desc(at, 1024u, 2), ds = mxp_desc(at + T::P_CODES, 1024u, 2);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t atom = FMT == MX_E2M1 ? i >> 1 : 0u, id = FMT == MX_E2M1 ? (i & 1u) * 2u : i;
+                    mxp_mma<FMT>(tmem, dp + 2u * i, ds + 2u * i, idesc0 | id << 4 | id << 29, cp + 4u * atom, cs + 4u * T::S_BLOCKS * atom, k != k0 || i != 0u);
+                }
+                mxp_commit(&ctl->empty[slot]);
             }
-            const uint64_t dp = mxp_desc(at, 1024u, 2), ds = mxp_desc(at + T::P_CODES, 1024u, 2);
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t atom = FMT == MX_E2M1 ? i >> 1 : 0u, id = FMT == MX_E2M1 ? (i & 1u) * 2u : i;
-                mxp_mma<FMT>(tmem, dp + 2u * i, ds + 2u * i, idesc0 | id << 4 | id << 29, cp + 4u * atom, cs + 4u * T::S_BLOCKS * atom,
-                             (n | i) != 0u);
-            }
-            mxp_commit(&ctl->empty[slot]);
+            mxp_commit(&ctl->done);
         }
-        mxp_commit(&ctl->done);
-        if (!ok) mxp_wait(&ctl->done, 0, ctl);                     // (what has been issued ends before the tensor memory goes)
+        if (!ok && made > 0u) mxp_wait(&ctl->done, (made - 1u) & 1u, ctl);      // (what has been issued ends before the tensor memory goes)
+    } else if (warp < 4u * T::HALVES) {
+        // ---- the way out: a warp has a quarter of the lanes, and all columns or half of them ----
+        const uint32_t row = (warp & 3u) * 32u + lane, c0 = (warp >> 2) * T::MINE;
+        const uint32_t from = tmem + ((warp & 3u) << 21) + c0;          // its first lane in the upper half of the address
+        uint32_t made = 0;
+        for (uint32_t tile = first; tile < p.tiles; tile += step, ++made) {
+            const uint32_t p0 = tile % p.tiles_p * 128u, s0 = tile / p.tiles_p * BN;
+            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            good = good && !*(volatile uint32_t*)&ctl->failed;
+            uint32_t raw[(T::MINE + 31u) / 32u][32];
+            __syncwarp();
+#pragma unroll
+            for (uint32_t c = 0; c < T::MINE; c += 32u) {
+                if (T::MINE < 32u) mxp_load16(from, raw[0]);
+                else mxp_load32(from + c, raw[c / 32u]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl->taken);
+#pragma unroll
+            for (uint32_t c = 0; c < T::MINE; c += 32u) {
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = (T::MINE >= 32u || i < 16) ? (good ? __uint_as_float(raw[c / 32u][i]) : __uint_as_float(0x7FC00000u)) : 0.f;
+                if (p.split == 1u) {
+                    mxp_out_any(p, p0 + row, s0 + c0 + c, min(T::MINE, 32u), v);
+                } else {
+                    float* part = reinterpret_cast<float*>(ring);       // [column][lane]; all copies and products are through
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (T::MINE >= 32u || i < 16) part[(c0 + c + i) * 128u + row] = v[i];
+                }
+            }
+        }
     }
     __syncwarp();
-
-    // ---- the way out: warps 0..3, each its quarter of the lanes ----
-    bool good = true;
-    const uint32_t quarter = tmem + (warp << 21);                 // lane 32 * warp in the upper half of the address
-    const uint32_t row = warp * 32u + lane;
-    float v[32];
-    if (warp < 4) {
-        good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, 0, ctl));
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        good = good && !*(volatile uint32_t*)&ctl->failed;
-        if (p.split == 1u) {
-            for (uint32_t c = 0; c < BN; c += 32u) {
-                uint32_t raw[32];
-                __syncwarp();
-                if (BN < 32u) mxp_load16(quarter + c, raw);
-                else mxp_load32(quarter + c, raw);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = (BN >= 32u || i < 16) ? (good ? __uint_as_float(raw[i]) : __uint_as_float(0x7FC00000u)) : 0.f;
-                mxp_out_any(p, p0 + row, s0 + c, min(BN, 32u), v);
-            }
-        } else {
-            float* part = reinterpret_cast<float*>(ring);           // [column][lane]; all copies and products are through
-            for (uint32_t c = 0; c < BN; c += 32u) {
-                uint32_t raw[32];
-                __syncwarp();
-                if (BN < 32u) mxp_load16(quarter + c, raw);
-                else mxp_load32(quarter + c, raw);
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (BN >= 32u || i < 16) part[(c + i) * 128u + row] = good ? __uint_as_float(raw[i]) : __uint_as_float(0x7FC00000u);
-            }
-        }
-    }
     if (p.split > 1u) {
         cluster_sync_all();
-        if (warp < 4) {
-            const uint32_t share = BN / p.split, c0 = rank * share;        // (a power of two of at least 2)
+        if (warp < 4) {                                                    // (a cluster has one tile)
+            const uint32_t share = BN / p.split, c0 = rank * share, row = warp * 32u + lane;        // (share: a power of two of at least 2)
+            const uint32_t p0 = first % p.tiles_p * 128u, s0 = first / p.tiles_p * BN;
             const uint32_t mine = smem_u32(ring) + (c0 * 128u + row) * 4u;
             for (uint32_t c = 0; c < share; c += 32u) {
                 const uint32_t n = min(share - c, 32u);
+                float v[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     float sum = 0.f;
@@ -345,7 +356,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 5) {
+    if (warp == MXP_ISSUER) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(T::COLUMNS));
     }
@@ -433,9 +444,11 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     uint32_t split = 1;
     while (bn < 256u && split < 8u && tiles * split * 2u <= 160u && p.p.s.stages >= 4u * split) split *= 2u;
     p.split = split;
-    if (tiles * split >= (1ull << 31)) return DIV_ERR_SHAPE;
-    return format == MX_E4M3 ? product_by_width<MX_E4M3>(bn, p, (uint32_t)(tiles * split), (cudaStream_t)cuda_stream)
-                             : product_by_width<MX_E2M1>(bn, p, (uint32_t)(tiles * split), (cudaStream_t)cuda_stream);
+    if (tiles >= (1ull << 31)) return DIV_ERR_SHAPE;
+    p.tiles = (uint32_t)tiles;
+    const uint32_t grid = split > 1u ? (uint32_t)tiles * split : (uint32_t)(tiles < MXP_SMS ? tiles : MXP_SMS);
+    return format == MX_E4M3 ? product_by_width<MX_E4M3>(bn, p, grid, (cudaStream_t)cuda_stream)
+                             : product_by_width<MX_E2M1>(bn, p, grid, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

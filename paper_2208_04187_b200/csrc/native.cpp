@@ -5,11 +5,15 @@
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+
+#include <pybind11/pybind11.h>
 
 #include <cstring>
 
@@ -108,77 +112,278 @@ PyObject* decompress(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---------------------------------------------------------------------------------------------
 // the operators of language models: outputs are new tensors on the inputs' device, the work goes to that device's current stream.  What
-// does not fit (device, dtype, shape) is a ValueError; a status of the library comes back as a number.
+// does not fit (device, dtype, shape) is a ValueError; a status of the library comes back as a number.  Their gradients are nodes
+// of the autograd graph in C++ (the Python form costs 60 us a step, more than most small steps compute).
 // ---------------------------------------------------------------------------------------------
-PyObject* refuse(const char* why) {
-    PyErr_SetString(PyExc_ValueError, why);
-    return nullptr;
+using at::Tensor;
+using torch::autograd::AutogradContext;
+using torch::autograd::Function;
+using torch::autograd::variable_list;
+
+struct Status : std::runtime_error {
+    div_status code;
+    explicit Status(div_status c) : std::runtime_error(div_status_string(c)), code(c) {}
+};
+void check(div_status s) {
+    if (s != DIV_OK) throw Status(s);
 }
 int lm_type(at::ScalarType t) { return t == at::kFloat ? DIV_F32 : t == at::kBFloat16 ? DIV_BF16 : t == at::kHalf ? DIV_F16 : -1; }
 // a matrix whose rows are runs of neighbours; anything else (a transposed one, a row repeated by expand) is copied
-at::Tensor by_rows(const at::Tensor& t) {
+Tensor by_rows(const Tensor& t) {
     const bool runs = (t.size(1) <= 1 || t.stride(1) == 1) && (t.size(0) <= 1 || t.stride(0) >= t.size(1));
     return runs ? t : t.contiguous();
 }
-bool matrix(const at::Tensor& t) { return t.is_cuda() && t.dim() == 2 && lm_type(t.scalar_type()) >= 0; }
-bool maybe_tensor(PyObject* o, const at::Tensor** out) {
-    *out = nullptr;
-    return o == Py_None || tensor_arg(o, out);
+void matrix(const Tensor& t, const char* what) {
+    TORCH_CHECK_VALUE(t.is_cuda() && t.dim() == 2 && lm_type(t.scalar_type()) >= 0, what, " must be a CUDA matrix of float32, bfloat16 or float16");
+}
+void* at_(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+size_t bytes_of(const Tensor& t) { return t.defined() ? (size_t)t.numel() : 0; }
+Tensor new_blob(const Tensor& like, int64_t rows, int64_t cols, int64_t format) {
+    div_mx_layout lo;
+    check(div_mx_bytes(rows, cols, (int32_t)format, &lo));
+    return at::empty({(int64_t)lo.total_bytes}, like.options().dtype(at::kByte));
+}
+
+struct Quantised {
+    Tensor rows, cols;
+};
+Quantised quantise(const Tensor& given, int64_t format, bool rows, bool cols) {
+    matrix(given, "x");
+    const c10::cuda::CUDAGuard guard(given.device());
+    // a transposed matrix: its rows are the columns of what lies in memory
+    const bool turned = given.stride(0) == 1 && given.stride(1) != 1 && given.stride(1) >= given.size(0);
+    const Tensor x = turned ? given.t() : by_rows(given);
+    if (turned) std::swap(rows, cols);
+    Quantised q;
+    if (rows) q.rows = new_blob(x, x.size(0), x.size(1), format);
+    if (cols) q.cols = new_blob(x, x.size(1), x.size(0), format);
+    check(div_mx_quantize(x.data_ptr(), x.size(0), x.size(1), x.stride(0), lm_type(x.scalar_type()), (int32_t)format, at_(q.rows), bytes_of(q.rows), at_(q.cols),
+                          bytes_of(q.cols), stream()));
+    if (turned) std::swap(q.rows, q.cols);
+    return q;
+}
+void blob_fits(const Tensor& t) {
+    TORCH_CHECK_VALUE(t.is_cuda() && t.is_contiguous() && t.scalar_type() == at::kByte, "a blob is a contiguous CUDA tensor of bytes");
+}
+Tensor product(const Tensor& a, int64_t m, const Tensor& b, int64_t n, int64_t k, int64_t format, at::ScalarType type) {
+    blob_fits(a);
+    blob_fits(b);
+    TORCH_CHECK_VALUE(a.device() == b.device(), "both operands must be on one device");
+    const c10::cuda::CUDAGuard guard(a.device());
+    Tensor out = at::empty({m, n}, a.options().dtype(type));
+    check(div_mx_matmul(a.data_ptr(), bytes_of(a), b.data_ptr(), bytes_of(b), m, n, k, (int32_t)format, out.data_ptr(), n, lm_type(type), stream()));
+    return out;
+}
+
+struct Normed {
+    Tensor y, blob, h, rstd;           // h: undefined without a residual
+};
+Normed norm(const Tensor& x0, const Tensor& r0, const Tensor& w0, double eps, bool want_y, int64_t format, bool want_rstd) {
+    matrix(x0, "x");
+    TORCH_CHECK_VALUE(!r0.defined() || (r0.device() == x0.device() && r0.scalar_type() == x0.scalar_type() && r0.sizes() == x0.sizes()),
+                      "residual must be like x: device, dtype and shape");
+    TORCH_CHECK_VALUE(w0.device() == x0.device() && w0.dim() == 1 && w0.size(0) == x0.size(1) && (w0.scalar_type() == x0.scalar_type() || w0.scalar_type() == at::kFloat),
+                      "weight must have one number a column, x's dtype or float32, on x's device");
+    const c10::cuda::CUDAGuard guard(x0.device());
+    const Tensor x = by_rows(x0), r = r0.defined() ? by_rows(r0) : Tensor(), w = w0.contiguous();
+    const int64_t rows = x.size(0), cols = x.size(1);
+    Normed n;
+    if (want_y) n.y = at::empty({rows, cols}, x.options());
+    if (format >= 0) n.blob = new_blob(x, rows, cols, format);
+    if (r.defined()) n.h = at::empty({rows, cols}, x.options());
+    if (want_rstd) n.rstd = at::empty({rows}, x.options().dtype(at::kFloat));
+    check(div_rms_norm_forward(x.data_ptr(), x.stride(0), at_(r), r.defined() ? r.stride(0) : 0, w.data_ptr(), lm_type(w.scalar_type()), rows, cols,
+                               lm_type(x.scalar_type()), (float)eps, at_(n.h), at_(n.y), at_(n.blob), bytes_of(n.blob), (int32_t)format, (float*)at_(n.rstd),
+                               stream()));
+    return n;
+}
+struct NormGrads {
+    Tensor dx, dw;
+};
+NormGrads norm_backward(const Tensor& dy0, const Tensor& dh0, const Tensor& h0, const Tensor& w0, const Tensor& rstd, bool want_dw) {
+    for (const Tensor* t : {&dy0, &dh0})
+        TORCH_CHECK_VALUE(!t->defined() || (t->device() == h0.device() && t->scalar_type() == h0.scalar_type() && t->sizes() == h0.sizes()),
+                          "gradients must be like h: device, dtype and shape");
+    const c10::cuda::CUDAGuard guard(h0.device());
+    const Tensor dy = by_rows(dy0), dh = dh0.defined() ? by_rows(dh0) : Tensor(), h = by_rows(h0), w = w0.contiguous();
+    const int64_t rows = h.size(0), cols = h.size(1);
+    NormGrads g;
+    g.dx = at::empty({rows, cols}, h.options());
+    Tensor ws;
+    if (want_dw) {
+        uint64_t bytes = 0;
+        check(div_rms_norm_workspace(rows, cols, &bytes));
+        ws = at::empty({(int64_t)bytes}, h.options().dtype(at::kByte));
+        g.dw = at::empty({cols}, w.options());
+    }
+    check(div_rms_norm_backward(dy.data_ptr(), dy.stride(0), at_(dh), dh.defined() ? dh.stride(0) : 0, h.data_ptr(), h.stride(0), w.data_ptr(),
+                                lm_type(w.scalar_type()), (const float*)rstd.data_ptr(), rows, cols, lm_type(h.scalar_type()), g.dx.data_ptr(), at_(g.dw), at_(ws),
+                                bytes_of(ws), stream()));
+    return g;
+}
+
+struct Logprobs {
+    Tensor logprobs, entropy, stats, top, indices;
+};
+Logprobs logprobs(const Tensor& x0, const Tensor& t0, int64_t top) {
+    matrix(x0, "logits");
+    TORCH_CHECK_VALUE(t0.device() == x0.device() && t0.scalar_type() == at::kLong && t0.dim() == 1 && t0.size(0) == x0.size(0),
+                      "targets must hold one int64 a row, on the logits' device");
+    TORCH_CHECK_VALUE(top >= 0 && top <= 32 && top <= x0.size(1), "top must lie between 0 and 32 and not pass the vocabulary");
+    const c10::cuda::CUDAGuard guard(x0.device());
+    const Tensor x = by_rows(x0), t = t0.contiguous();
+    const int64_t rows = x.size(0);
+    const auto f32 = x.options().dtype(at::kFloat);
+    Logprobs l = {at::empty({rows}, f32), at::empty({rows}, f32), at::empty({rows, 2}, f32), at::empty({rows, top}, f32), at::empty({rows, top}, t.options())};
+    check(div_token_logprobs_forward(x.data_ptr(), x.stride(0), rows, x.size(1), lm_type(x.scalar_type()), t.data_ptr<int64_t>(), (int32_t)top,
+                                     l.logprobs.data_ptr<float>(), l.entropy.data_ptr<float>(), l.stats.data_ptr<float>(), l.top.data_ptr<float>(),
+                                     l.indices.data_ptr<int64_t>(), stream()));
+    return l;
+}
+
+// ---- gradients ----
+// what a backward pass gives has no gradient of its own: asking for one is an error, not a zero
+variable_list once(variable_list&& out) {
+    if (!at::GradMode::is_enabled()) return std::move(out);
+    variable_list some;
+    for (const Tensor& t : out)
+        if (t.defined()) some.push_back(t);
+    if (some.empty()) return std::move(out);
+    auto error = std::make_shared<torch::autograd::DelayedError>("the gradient of this operator has no gradient", (int64_t)some.size());
+    for (Tensor& t : some) t = t.detach().requires_grad_();                                   // (the node wants inputs that ask for one)
+    variable_list marked = (*error)(std::move(some));
+    size_t k = 0;
+    for (Tensor& t : out)
+        if (t.defined()) t = marked[k++];
+    return std::move(out);
+}
+
+struct LinearFn : Function<LinearFn> {                       // y = Q(x) Q(w)^T, dx = Q(dy) Q(w^T)^T, dw = Q(dy^T) Q(x^T)^T
+    static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, int64_t format) {
+        const Quantised qx = quantise(x, format, true, w.requires_grad()), qw = quantise(w, format, true, x.requires_grad());
+        ctx->save_for_backward({qx.cols, qw.cols});          // of the input and the weight the quantised columns alone
+        ctx->saved_data["format"] = format;
+        ctx->saved_data["types"] = std::vector<int64_t>{(int64_t)x.scalar_type(), (int64_t)w.scalar_type()};
+        ctx->saved_data["sizes"] = std::vector<int64_t>{x.size(0), w.size(0), x.size(1)};
+        return product(qx.rows, x.size(0), qw.rows, w.size(0), x.size(1), format, x.scalar_type());
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        if (!g[0].defined()) return {Tensor(), Tensor(), Tensor()};
+        const variable_list kept = ctx->get_saved_variables();
+        const int64_t format = ctx->saved_data["format"].toInt();
+        const auto types = ctx->saved_data["types"].toIntVector(), sizes = ctx->saved_data["sizes"].toIntVector();
+        const int64_t m = sizes[0], n = sizes[1], k = sizes[2];
+        const bool need_x = ctx->needs_input_grad(0) && kept[1].defined(), need_w = ctx->needs_input_grad(1) && kept[0].defined();
+        Tensor dx, dw;
+        if (need_x || need_w) {
+            const Quantised q = quantise(g[0], format, need_x, need_w);
+            if (need_x) dx = product(q.rows, m, kept[1], k, n, format, (at::ScalarType)types[0]);
+            if (need_w) dw = product(q.cols, n, kept[0], k, m, format, (at::ScalarType)types[1]);
+        }
+        return once({dx, dw, Tensor()});
+    }
+};
+
+struct NormFn : Function<NormFn> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& x, const std::optional<Tensor>& given, const Tensor& w, double eps) {
+        const Tensor r = given ? *given : Tensor();
+        Normed n = norm(x, r, w, eps, true, -1, true);
+        ctx->save_for_backward({r.defined() ? n.h : x, w, n.rstd});
+        ctx->set_materialize_grads(false);
+        if (!r.defined()) return {n.y};
+        return {n.y, n.h};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        const bool fused = g.size() > 1;
+        const Tensor dh = fused ? g[1] : Tensor();
+        if (!g[0].defined()) return {dh, fused ? dh : Tensor(), Tensor(), Tensor()};
+        const variable_list kept = ctx->get_saved_variables();
+        const NormGrads d = norm_backward(g[0], dh, kept[0], kept[1], kept[2], ctx->needs_input_grad(2 - !fused));
+        variable_list out = once({d.dx, d.dw});
+        return {out[0], fused ? out[0] : Tensor(), out[1], Tensor()};
+    }
+};
+
+// The norm's output goes into the product in few bits and is not kept: backward makes it again from h and rstd.
+struct NormLinearFn : Function<NormLinearFn> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& x, const std::optional<Tensor>& given, const Tensor& g, const Tensor& w, double eps, int64_t format) {
+        const Tensor r = given ? *given : Tensor();
+        Normed n = norm(x, r, g, eps, false, format, true);
+        const Quantised qw = quantise(w, format, true, true);
+        ctx->save_for_backward({r.defined() ? n.h : x, g, n.rstd, qw.cols});
+        ctx->set_materialize_grads(false);
+        ctx->saved_data["format"] = format;
+        ctx->saved_data["eps"] = eps;
+        ctx->saved_data["type"] = (int64_t)w.scalar_type();
+        ctx->saved_data["outs"] = w.size(0);
+        Tensor out = product(n.blob, x.size(0), qw.rows, w.size(0), x.size(1), format, x.scalar_type());
+        if (!r.defined()) return {out};
+        return {out, n.h};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        const bool fused = g.size() > 1;
+        const Tensor dh = fused ? g[1] : Tensor();
+        if (!g[0].defined()) return {dh, fused ? dh : Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        const variable_list kept = ctx->get_saved_variables();
+        const Tensor &h = kept[0], &weight = kept[1], &rstd = kept[2];
+        const int64_t format = ctx->saved_data["format"].toInt(), n = ctx->saved_data["outs"].toInt(), m = h.size(0), k = h.size(1);
+        const int at = 1 + fused;                             // of the norm's weight among the inputs that are there
+        const bool need_w = ctx->needs_input_grad(at + 1);
+        const Quantised q = quantise(g[0], format, true, need_w);
+        Tensor dw;
+        if (need_w) {
+            const Normed y = norm(h, Tensor(), weight, ctx->saved_data["eps"].toDouble(), true, -1, false);
+            dw = product(q.cols, n, quantise(y.y, format, false, true).cols, k, m, format, (at::ScalarType)ctx->saved_data["type"].toInt());
+        }
+        const Tensor dy = product(q.rows, m, kept[3], k, n, format, h.scalar_type());
+        const NormGrads d = norm_backward(dy, dh, h, weight, rstd, ctx->needs_input_grad(at));
+        variable_list out = once({d.dx, d.dw, dw});
+        return {out[0], fused ? out[0] : Tensor(), out[1], out[2], Tensor(), Tensor()};
+    }
+};
+
+struct LogprobsFn : Function<LogprobsFn> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& x, const Tensor& t, int64_t top) {
+        Logprobs l = logprobs(x, t, top);
+        ctx->save_for_backward({x, t, l.stats, l.entropy});
+        ctx->mark_non_differentiable({l.top, l.indices});
+        ctx->set_materialize_grads(false);
+        return {l.logprobs, l.entropy, l.top, l.indices};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list g) {
+        if (!g[0].defined() && !g[1].defined()) return {Tensor(), Tensor(), Tensor()};
+        const variable_list kept = ctx->get_saved_variables();
+        const c10::cuda::CUDAGuard guard(kept[0].device());
+        const Tensor x = by_rows(kept[0]), t = kept[1].contiguous(), dl = g[0].defined() ? g[0].contiguous() : Tensor(), de = g[1].defined() ? g[1].contiguous() : Tensor();
+        Tensor out = at::empty({x.size(0), x.size(1)}, x.options());
+        check(div_token_logprobs_backward(x.data_ptr(), x.stride(0), x.size(0), x.size(1), lm_type(x.scalar_type()), t.data_ptr<int64_t>(),
+                                          kept[2].data_ptr<float>(), kept[3].data_ptr<float>(), (const float*)at_(dl), (const float*)at_(de), out.data_ptr(), stream()));
+        return once({out, Tensor(), Tensor()});
+    }
+};
+
+// ---- the calls ----
+bool wants_grad(std::initializer_list<const Tensor*> all) {
+    if (!at::GradMode::is_enabled()) return false;
+    for (const Tensor* t : all)
+        if (t->defined() && t->requires_grad()) return true;
+    return false;
+}
+bool maybe_tensor(PyObject* o, Tensor* out) {
+    const Tensor* t = nullptr;
+    if (o == Py_None) return true;
+    if (!tensor_arg(o, &t)) return false;
+    *out = *t;
+    return true;
 }
 bool number(PyObject* o, int64_t* out) {
     *out = PyLong_AsLongLong(o);
     return !(*out == -1 && PyErr_Occurred());
 }
-PyObject* or_none(at::Tensor&& t) {
-    if (t.defined()) return THPVariable_Wrap(std::move(t));
-    Py_RETURN_NONE;
+bool real(PyObject* o, double* out) {
+    *out = PyFloat_AsDouble(o);
+    return !(*out == -1.0 && PyErr_Occurred());
 }
-at::Tensor new_blob(const at::Tensor& like, int64_t rows, int64_t cols, int64_t format, div_status* st) {
-    div_mx_layout lo;
-    *st = div_mx_bytes(rows, cols, (int32_t)format, &lo);
-    return *st == DIV_OK ? at::empty({(int64_t)lo.total_bytes}, like.options().dtype(at::kByte)) : at::Tensor();
-}
-// the call itself, without the interpreter (a full launch queue blocks)
-template <typename F> div_status released(F&& f) {
-    div_status got;
-    Py_BEGIN_ALLOW_THREADS
-    got = f();
-    Py_END_ALLOW_THREADS
-    return got;
-}
-
-// mx_quantize(x, format, rows?, columns?) -> (blob by rows or None, blob by columns or None)
-PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    HANDLE_TH_ERRORS
-    const at::Tensor* given;
-    int64_t format;
-    if (n != 4) return refuse("mx_quantize takes 4 arguments");
-    if (!tensor_arg(a[0], &given) || !number(a[1], &format)) return nullptr;
-    if (!matrix(*given)) return refuse("x must be a CUDA matrix of float32, bfloat16 or float16");
-    bool rows = a[2] == Py_True, cols = a[3] == Py_True;
-    const c10::cuda::CUDAGuard guard(given->device());
-    // a transposed matrix: its rows are the columns of what lies in memory
-    const bool turned = given->stride(0) == 1 && given->stride(1) != 1 && given->stride(1) >= given->size(0);
-    const at::Tensor x = turned ? given->t() : by_rows(*given);
-    if (turned) std::swap(rows, cols);
-    div_status st = DIV_OK, st2 = DIV_OK;
-    at::Tensor r, c;
-    if (rows) r = new_blob(x, x.size(0), x.size(1), format, &st);
-    if (cols) c = new_blob(x, x.size(1), x.size(0), format, &st2);
-    if (st != DIV_OK || st2 != DIV_OK) return PyLong_FromLong((long)(st ? st : st2));
-    const void* from = x.data_ptr();
-    void *to_r = rows ? r.data_ptr() : nullptr, *to_c = cols ? c.data_ptr() : nullptr, *on = stream();
-    st = released([&] {
-        return div_mx_quantize(from, x.size(0), x.size(1), x.stride(0), lm_type(x.scalar_type()), (int32_t)format, to_r, rows ? (size_t)r.numel() : 0, to_c,
-                               cols ? (size_t)c.numel() : 0, on);
-    });
-    if (st != DIV_OK) return PyLong_FromLong((long)st);
-    if (turned) std::swap(r, c);
-    PyObject *pr = or_none(std::move(r)), *pc = or_none(std::move(c));
-    return pr && pc ? Py_BuildValue("NN", pr, pc) : nullptr;
-    END_HANDLE_TH_ERRORS
-}
-
 bool dtype_arg(PyObject* o, at::ScalarType* out) {
     if (!THPDtype_Check(o)) {
         PyErr_SetString(PyExc_TypeError, "expected a dtype");
@@ -191,181 +396,200 @@ bool dtype_arg(PyObject* o, at::ScalarType* out) {
     }
     return true;
 }
+bool count_is(Py_ssize_t n, Py_ssize_t want) {
+    if (n != want) PyErr_Format(PyExc_TypeError, "takes %zd arguments", want);
+    return n == want;
+}
+PyObject* wrapped(std::initializer_list<Tensor> all) {             // a tuple; None for what is not there
+    PyObject* out = PyTuple_New((Py_ssize_t)all.size());
+    Py_ssize_t i = 0;
+    for (const Tensor& t : all) {
+        PyObject* o = nullptr;
+        if (out) o = t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None);
+        if (!o) {
+            Py_XDECREF(out);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(out, i++, o);
+    }
+    return out;
+}
+// runs f without the interpreter (a full launch queue blocks); false: the library's status is in *code
+template <typename F> bool ran(div_status* code, F&& f) {
+    pybind11::gil_scoped_release released;
+    try {
+        f();
+        return true;
+    } catch (const Status& s) {
+        *code = s.code;
+        return false;
+    }
+}
+
+// mx_quantize(x, format, rows?, columns?) -> (blob by rows or None, blob by columns or None)
+PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Tensor* x;
+    int64_t format;
+    if (!count_is(n, 4) || !tensor_arg(a[0], &x) || !number(a[1], &format)) return nullptr;
+    const bool rows = a[2] == Py_True, cols = a[3] == Py_True;
+    Quantised q;
+    div_status st;
+    const Tensor given = *x;
+    if (!ran(&st, [&] { q = quantise(given, format, rows, cols); })) return PyLong_FromLong((long)st);
+    return wrapped({q.rows, q.cols});
+    END_HANDLE_TH_ERRORS
+}
 
 // mx_dequantize(blob, rows, cols, format, dtype) -> matrix
 PyObject* mx_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    const at::Tensor* blob;
+    const Tensor* b;
     int64_t rows, cols, format;
     at::ScalarType type;
-    if (n != 5) return refuse("mx_dequantize takes 5 arguments");
-    if (!tensor_arg(a[0], &blob) || !number(a[1], &rows) || !number(a[2], &cols) || !number(a[3], &format) || !dtype_arg(a[4], &type)) return nullptr;
-    if (!blob->is_cuda() || !blob->is_contiguous() || blob->scalar_type() != at::kByte) return refuse("a blob is a contiguous CUDA tensor of bytes");
-    const c10::cuda::CUDAGuard guard(blob->device());
-    at::Tensor out = at::empty({rows, cols}, blob->options().dtype(type));
-    const void* from = blob->data_ptr();
-    void *to = out.data_ptr(), *on = stream();
-    const div_status st = released([&] { return div_mx_dequantize(from, (size_t)blob->numel(), rows, cols, (int32_t)format, to, lm_type(type), on); });
-    return st == DIV_OK ? THPVariable_Wrap(std::move(out)) : PyLong_FromLong((long)st);
+    if (!count_is(n, 5) || !tensor_arg(a[0], &b) || !number(a[1], &rows) || !number(a[2], &cols) || !number(a[3], &format) || !dtype_arg(a[4], &type)) return nullptr;
+    const Tensor blob = *b;
+    Tensor out;
+    div_status st;
+    if (!ran(&st, [&] {
+            blob_fits(blob);
+            const c10::cuda::CUDAGuard guard(blob.device());
+            out = at::empty({rows, cols}, blob.options().dtype(type));
+            check(div_mx_dequantize(blob.data_ptr(), bytes_of(blob), rows, cols, (int32_t)format, out.data_ptr(), lm_type(type), stream()));
+        }))
+        return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(std::move(out));
     END_HANDLE_TH_ERRORS
 }
 
 // mx_matmul(blob a, m, blob b, n, k, format, dtype) -> m x n
 PyObject* mx_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    const at::Tensor *p, *q;
+    const Tensor *p, *q;
     int64_t m, cols, k, format;
     at::ScalarType type;
-    if (n != 7) return refuse("mx_matmul takes 7 arguments");
-    if (!tensor_arg(a[0], &p) || !number(a[1], &m) || !tensor_arg(a[2], &q) || !number(a[3], &cols) || !number(a[4], &k) || !number(a[5], &format) ||
-        !dtype_arg(a[6], &type))
+    if (!count_is(n, 7) || !tensor_arg(a[0], &p) || !number(a[1], &m) || !tensor_arg(a[2], &q) || !number(a[3], &cols) || !number(a[4], &k) ||
+        !number(a[5], &format) || !dtype_arg(a[6], &type))
         return nullptr;
-    for (const at::Tensor* t : {p, q})
-        if (!t->is_cuda() || !t->is_contiguous() || t->scalar_type() != at::kByte) return refuse("a blob is a contiguous CUDA tensor of bytes");
-    if (p->device() != q->device()) return refuse("both operands must be on one device");
-    const c10::cuda::CUDAGuard guard(p->device());
-    at::Tensor out = at::empty({m, cols}, p->options().dtype(type));
-    const void *pa = p->data_ptr(), *pb = q->data_ptr();
-    void *to = out.data_ptr(), *on = stream();
-    const div_status st = released([&] {
-        return div_mx_matmul(pa, (size_t)p->numel(), pb, (size_t)q->numel(), m, cols, k, (int32_t)format, to, cols, lm_type(type), on);
-    });
-    return st == DIV_OK ? THPVariable_Wrap(std::move(out)) : PyLong_FromLong((long)st);
+    const Tensor left = *p, right = *q;
+    Tensor out;
+    div_status st;
+    if (!ran(&st, [&] { out = product(left, m, right, cols, k, format, type); })) return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(std::move(out));
     END_HANDLE_TH_ERRORS
 }
 
-// rms_norm_forward(x, residual or None, weight, eps, y?, format or -1, rstd?) -> (y, blob, h, rstd), each or None; h is None without a residual
-PyObject* rms_norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// mx_linear(x, w, format) -> y
+PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    const at::Tensor *x0, *r0, *w0;
+    const Tensor *p, *q;
     int64_t format;
-    if (n != 7) return refuse("rms_norm_forward takes 7 arguments");
-    if (!tensor_arg(a[0], &x0) || !maybe_tensor(a[1], &r0) || !tensor_arg(a[2], &w0) || !number(a[5], &format)) return nullptr;
-    const double eps = PyFloat_AsDouble(a[3]);
-    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
-    if (!matrix(*x0)) return refuse("x must be a CUDA matrix of float32, bfloat16 or float16");
-    if (r0 && (r0->device() != x0->device() || r0->scalar_type() != x0->scalar_type() || r0->sizes() != x0->sizes()))
-        return refuse("residual must be like x: device, dtype and shape");
-    if (w0->device() != x0->device() || w0->dim() != 1 || w0->size(0) != x0->size(1) || !(w0->scalar_type() == x0->scalar_type() || w0->scalar_type() == at::kFloat))
-        return refuse("weight must have one number a column, x's dtype or float32, on x's device");
-    const c10::cuda::CUDAGuard guard(x0->device());
-    const at::Tensor x = by_rows(*x0), res = r0 ? by_rows(*r0) : at::Tensor(), w = w0->contiguous();
-    const int64_t rows = x.size(0), cols = x.size(1);
-    at::Tensor y, blob, h, rstd;
-    div_status st = DIV_OK;
-    if (a[4] == Py_True) y = at::empty({rows, cols}, x.options());
-    if (format >= 0) blob = new_blob(x, rows, cols, format, &st);
-    if (st != DIV_OK) return PyLong_FromLong((long)st);
-    if (r0) h = at::empty({rows, cols}, x.options());
-    if (a[6] == Py_True) rstd = at::empty({rows}, x.options().dtype(at::kFloat));
-    const auto at_ = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
-    const void *px = x.data_ptr(), *pr = at_(res), *pw = w.data_ptr();
-    void *ph = at_(h), *py = at_(y), *pb = at_(blob), *ps = at_(rstd), *on = stream();
-    st = released([&] {
-        return div_rms_norm_forward(px, x.stride(0), pr, r0 ? res.stride(0) : 0, pw, lm_type(w.scalar_type()), rows, cols, lm_type(x.scalar_type()), (float)eps, ph,
-                                    py, pb, blob.defined() ? (size_t)blob.numel() : 0, (int32_t)format, (float*)ps, on);
-    });
-    if (st != DIV_OK) return PyLong_FromLong((long)st);
-    PyObject *o0 = or_none(std::move(y)), *o1 = or_none(std::move(blob)), *o2 = or_none(std::move(h)), *o3 = or_none(std::move(rstd));
-    return o0 && o1 && o2 && o3 ? Py_BuildValue("NNNN", o0, o1, o2, o3) : nullptr;
+    if (!count_is(n, 3) || !tensor_arg(a[0], &p) || !tensor_arg(a[1], &q) || !number(a[2], &format)) return nullptr;
+    const Tensor x = *p, w = *q;
+    Tensor y;
+    div_status st;
+    if (!ran(&st, [&] {
+            if (wants_grad({&x, &w})) y = LinearFn::apply(x, w, format);
+            else y = product(quantise(x, format, true, false).rows, x.size(0), quantise(w, format, true, false).rows, w.size(0), x.size(1), format, x.scalar_type());
+        }))
+        return PyLong_FromLong((long)st);
+    return THPVariable_Wrap(std::move(y));
     END_HANDLE_TH_ERRORS
 }
 
-// rms_norm_backward(dy, dh or None, h, weight, rstd, dweight?) -> (dx, dweight or None)
-PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// rms_norm(x, residual or None, weight, eps) -> (y, h or None)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    const at::Tensor *dy0, *dh0, *h0, *w0, *s0;
-    if (n != 6) return refuse("rms_norm_backward takes 6 arguments");
-    if (!tensor_arg(a[0], &dy0) || !maybe_tensor(a[1], &dh0) || !tensor_arg(a[2], &h0) || !tensor_arg(a[3], &w0) || !tensor_arg(a[4], &s0)) return nullptr;
-    if (!matrix(*h0)) return refuse("h must be a CUDA matrix of float32, bfloat16 or float16");
-    for (const at::Tensor* t : {dy0, dh0})
-        if (t && (t->device() != h0->device() || t->scalar_type() != h0->scalar_type() || t->sizes() != h0->sizes()))
-            return refuse("gradients must be like h: device, dtype and shape");
-    if (w0->device() != h0->device() || w0->dim() != 1 || w0->size(0) != h0->size(1) || !(w0->scalar_type() == h0->scalar_type() || w0->scalar_type() == at::kFloat))
-        return refuse("weight must have one number a column, h's dtype or float32, on h's device");
-    if (s0->device() != h0->device() || s0->scalar_type() != at::kFloat || s0->dim() != 1 || s0->size(0) != h0->size(0) || !s0->is_contiguous())
-        return refuse("rstd must hold one float32 a row");
-    const c10::cuda::CUDAGuard guard(h0->device());
-    const at::Tensor dy = by_rows(*dy0), dh = dh0 ? by_rows(*dh0) : at::Tensor(), h = by_rows(*h0), w = w0->contiguous();
-    const int64_t rows = h.size(0), cols = h.size(1);
-    at::Tensor dx = at::empty({rows, cols}, h.options()), dw, ws;
-    if (a[5] == Py_True) {
-        uint64_t bytes = 0;
-        const div_status st = div_rms_norm_workspace(rows, cols, &bytes);
-        if (st != DIV_OK) return PyLong_FromLong((long)st);
-        ws = at::empty({(int64_t)bytes}, h.options().dtype(at::kByte));
-        dw = at::empty({cols}, w.options());
-    }
-    const void *pdy = dy.data_ptr(), *pdh = dh0 ? dh.data_ptr() : nullptr, *ph = h.data_ptr(), *pw = w.data_ptr(), *ps = s0->data_ptr();
-    void *pdx = dx.data_ptr(), *pdw = dw.defined() ? dw.data_ptr() : nullptr, *pws = ws.defined() ? ws.data_ptr() : nullptr, *on = stream();
-    const div_status st = released([&] {
-        return div_rms_norm_backward(pdy, dy.stride(0), pdh, dh0 ? dh.stride(0) : 0, ph, h.stride(0), pw, lm_type(w.scalar_type()), (const float*)ps, rows, cols,
-                                     lm_type(h.scalar_type()), pdx, pdw, pws, ws.defined() ? (size_t)ws.numel() : 0, on);
-    });
-    if (st != DIV_OK) return PyLong_FromLong((long)st);
-    PyObject *o0 = THPVariable_Wrap(std::move(dx)), *o1 = or_none(std::move(dw));
-    return o0 && o1 ? Py_BuildValue("NN", o0, o1) : nullptr;
+    const Tensor *p, *q;
+    Tensor r;
+    double eps;
+    if (!count_is(n, 4) || !tensor_arg(a[0], &p) || !maybe_tensor(a[1], &r) || !tensor_arg(a[2], &q) || !real(a[3], &eps)) return nullptr;
+    const Tensor x = *p, w = *q;
+    Tensor y, h;
+    div_status st;
+    if (!ran(&st, [&] {
+            if (wants_grad({&x, &r, &w})) {
+                const variable_list got = NormFn::apply(x, r.defined() ? std::optional<Tensor>(r) : std::nullopt, w, eps);
+                y = got[0];
+                if (got.size() > 1) h = got[1];
+            } else {
+                const Normed got = norm(x, r, w, eps, true, -1, false);
+                y = got.y;
+                h = got.h;
+            }
+        }))
+        return PyLong_FromLong((long)st);
+    return wrapped({y, h});
     END_HANDLE_TH_ERRORS
 }
 
-bool targets_fit(const at::Tensor& t, const at::Tensor& x) {
-    return t.device() == x.device() && t.scalar_type() == at::kLong && t.dim() == 1 && t.size(0) == x.size(0);
-}
-
-// token_logprobs_forward(logits, targets, top) -> (logprobs, entropy, stats, top log probabilities, top indices)
-PyObject* token_logprobs_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// rms_norm_mx(x, residual or None, weight, eps, format) -> (blob, h or None)
+PyObject* rms_norm_mx(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    const at::Tensor *x0, *t0;
-    int64_t top;
-    if (n != 3) return refuse("token_logprobs_forward takes 3 arguments");
-    if (!tensor_arg(a[0], &x0) || !tensor_arg(a[1], &t0) || !number(a[2], &top)) return nullptr;
-    if (!matrix(*x0)) return refuse("logits must be a CUDA matrix of float32, bfloat16 or float16");
-    if (!targets_fit(*t0, *x0)) return refuse("targets must hold one int64 a row, on the logits' device");
-    if (top < 0 || top > 32 || top > x0->size(1)) return refuse("top must lie between 0 and 32 and not pass the vocabulary");
-    const c10::cuda::CUDAGuard guard(x0->device());
-    const at::Tensor x = by_rows(*x0), t = t0->contiguous();
-    const int64_t rows = x.size(0);
-    const auto f32 = x.options().dtype(at::kFloat);
-    at::Tensor lp = at::empty({rows}, f32), ent = at::empty({rows}, f32), stats = at::empty({rows, 2}, f32), tv = at::empty({rows, top}, f32),
-               ti = at::empty({rows, top}, x.options().dtype(at::kLong));
-    const void *px = x.data_ptr(), *pt = t.data_ptr();
-    void *p0 = lp.data_ptr(), *p1 = ent.data_ptr(), *p2 = stats.data_ptr(), *p3 = tv.data_ptr(), *p4 = ti.data_ptr(), *on = stream();
-    const div_status st = released([&] {
-        return div_token_logprobs_forward(px, x.stride(0), rows, x.size(1), lm_type(x.scalar_type()), (const int64_t*)pt, (int32_t)top, (float*)p0, (float*)p1,
-                                          (float*)p2, (float*)p3, (int64_t*)p4, on);
-    });
-    if (st != DIV_OK) return PyLong_FromLong((long)st);
-    PyObject *o0 = THPVariable_Wrap(std::move(lp)), *o1 = THPVariable_Wrap(std::move(ent)), *o2 = THPVariable_Wrap(std::move(stats)),
-             *o3 = THPVariable_Wrap(std::move(tv)), *o4 = THPVariable_Wrap(std::move(ti));
-    return o0 && o1 && o2 && o3 && o4 ? Py_BuildValue("NNNNN", o0, o1, o2, o3, o4) : nullptr;
+    const Tensor *p, *q;
+    Tensor r;
+    double eps;
+    int64_t format;
+    if (!count_is(n, 5) || !tensor_arg(a[0], &p) || !maybe_tensor(a[1], &r) || !tensor_arg(a[2], &q) || !real(a[3], &eps) || !number(a[4], &format)) return nullptr;
+    const Tensor x = *p, w = *q;
+    Normed got;
+    div_status st;
+    if (!ran(&st, [&] { got = norm(x, r, w, eps, false, format, false); })) return PyLong_FromLong((long)st);
+    return wrapped({got.blob, got.h});
     END_HANDLE_TH_ERRORS
 }
 
-// token_logprobs_backward(logits, targets, stats, entropy, dlogprobs or None, dentropy or None) -> dlogits
-PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// mx_norm_linear(x, residual or None, norm weight, w, eps, format) -> (out, h or None)
+PyObject* mx_norm_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    const at::Tensor *x0, *t0, *s0, *e0, *dl0, *de0;
-    if (n != 6) return refuse("token_logprobs_backward takes 6 arguments");
-    if (!tensor_arg(a[0], &x0) || !tensor_arg(a[1], &t0) || !tensor_arg(a[2], &s0) || !tensor_arg(a[3], &e0) || !maybe_tensor(a[4], &dl0) ||
-        !maybe_tensor(a[5], &de0))
+    const Tensor *p, *q, *v;
+    Tensor r;
+    double eps;
+    int64_t format;
+    if (!count_is(n, 6) || !tensor_arg(a[0], &p) || !maybe_tensor(a[1], &r) || !tensor_arg(a[2], &q) || !tensor_arg(a[3], &v) || !real(a[4], &eps) ||
+        !number(a[5], &format))
         return nullptr;
-    if (!matrix(*x0)) return refuse("logits must be a CUDA matrix of float32, bfloat16 or float16");
-    if (!targets_fit(*t0, *x0)) return refuse("targets must hold one int64 a row, on the logits' device");
-    for (const at::Tensor* t : {s0, e0, dl0, de0})
-        if (t && (t->device() != x0->device() || t->scalar_type() != at::kFloat || t->dim() != (t == s0 ? 2 : 1) || t->size(0) != x0->size(0) ||
-                  (t == s0 && t->size(1) != 2)))
-            return refuse("stats, entropy and the gradients are float32, of the shapes that the forward pass gave");
-    const c10::cuda::CUDAGuard guard(x0->device());
-    const at::Tensor x = by_rows(*x0), t = t0->contiguous(), s = s0->contiguous(), e = e0->contiguous(), dl = dl0 ? dl0->contiguous() : at::Tensor(),
-                     de = de0 ? de0->contiguous() : at::Tensor();
-    at::Tensor out = at::empty({x.size(0), x.size(1)}, x.options());
-    const void *px = x.data_ptr(), *pt = t.data_ptr(), *ps = s.data_ptr(), *pe = e.data_ptr(), *pl = dl0 ? dl.data_ptr() : nullptr, *pd = de0 ? de.data_ptr() : nullptr;
-    void *to = out.data_ptr(), *on = stream();
-    const div_status st = released([&] {
-        return div_token_logprobs_backward(px, x.stride(0), x.size(0), x.size(1), lm_type(x.scalar_type()), (const int64_t*)pt, (const float*)ps, (const float*)pe,
-                                           (const float*)pl, (const float*)pd, to, on);
-    });
-    return st == DIV_OK ? THPVariable_Wrap(std::move(out)) : PyLong_FromLong((long)st);
+    const Tensor x = *p, g = *q, w = *v;
+    Tensor out, h;
+    div_status st;
+    if (!ran(&st, [&] {
+            if (wants_grad({&x, &r, &g, &w})) {
+                const variable_list got = NormLinearFn::apply(x, r.defined() ? std::optional<Tensor>(r) : std::nullopt, g, w, eps, format);
+                out = got[0];
+                if (got.size() > 1) h = got[1];
+            } else {
+                const Normed got = norm(x, r, g, eps, false, format, false);
+                h = got.h;
+                out = product(got.blob, x.size(0), quantise(w, format, true, false).rows, w.size(0), x.size(1), format, x.scalar_type());
+            }
+        }))
+        return PyLong_FromLong((long)st);
+    return wrapped({out, h});
+    END_HANDLE_TH_ERRORS
+}
+
+// token_logprobs(logits, targets, top) -> (logprobs, entropy, top log probabilities, top indices)
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Tensor *p, *q;
+    int64_t top;
+    if (!count_is(n, 3) || !tensor_arg(a[0], &p) || !tensor_arg(a[1], &q) || !number(a[2], &top)) return nullptr;
+    const Tensor x = *p, t = *q;
+    Logprobs l;
+    div_status st;
+    if (!ran(&st, [&] {
+            if (wants_grad({&x})) {
+                const variable_list got = LogprobsFn::apply(x, t, top);
+                l.logprobs = got[0];
+                l.entropy = got[1];
+                l.top = got[2];
+                l.indices = got[3];
+            } else {
+                l = logprobs(x, t, top);
+            }
+        }))
+        return PyLong_FromLong((long)st);
+    return wrapped({l.logprobs, l.entropy, l.top, l.indices});
     END_HANDLE_TH_ERRORS
 }
 
@@ -373,8 +597,8 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"compress", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(compress)), METH_FASTCALL, nullptr},
     {"decompress", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decompress)), METH_FASTCALL, nullptr},
-    CALL(mx_quantize), CALL(mx_dequantize), CALL(mx_matmul), CALL(rms_norm_forward), CALL(rms_norm_backward), CALL(token_logprobs_forward),
-    CALL(token_logprobs_backward),
+    CALL(mx_quantize), CALL(mx_dequantize), CALL(mx_matmul), CALL(mx_linear), CALL(rms_norm), CALL(rms_norm_mx), CALL(mx_norm_linear),
+    CALL(token_logprobs),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -13,7 +13,7 @@ backward pass is the quantised form of its input, 8.25 or 4.25 bits a number, an
 
 `DivisionLinear`, `DivisionRMSNorm` and `DivisionNormLinear` are the modules; `to_division_layers` puts them in place of torch's.
 
-Glue only, as in `autograd`: every step runs in the CUDA library through the C ABI (include/division.h says what it
+Glue only, as in `autograd`: every step, of backward passes too, runs in the CUDA library through the C ABI (include/division.h says what it
 computes), on the current stream of the inputs' device.  Inputs are CUDA tensors of dtype float32, bfloat16 or float16; leading
 dimensions are folded into rows.  Rows that are runs of neighbours are read where they are, whatever their stride.
 """
@@ -121,40 +121,6 @@ def mx_matmul(a: MxTensor, b: MxTensor, dtype=torch.bfloat16):
     return _call("mx_matmul", a.blob, a.rows, b.blob, b.rows, a.cols, _FORMATS[a.fmt], dtype)
 
 
-class _MxLinear(torch.autograd.Function):
-    """y = Q(x) Q(w)^T, dx = Q(dy) Q(w^T)^T, dw = Q(dy^T) Q(x^T)^T; kept for backward: x and w by columns."""
-
-    @staticmethod
-    def forward(ctx, x, w, fmt):
-        need_x, need_w = ctx.needs_input_grad[:2]
-        if need_w:
-            xr, ctx.xc = mx_quantize_both(x, fmt)
-        else:
-            xr, ctx.xc = mx_quantize(x, fmt), None
-        if need_x:
-            wr, ctx.wc = mx_quantize_both(w, fmt)
-        else:
-            wr, ctx.wc = mx_quantize(w, fmt), None
-        ctx.fmt, ctx.types = fmt, (x.dtype, w.dtype)
-        return mx_matmul(xr, wr, x.dtype)
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dy):
-        dx = dw = None
-        if ctx.wc is not None and ctx.xc is not None:
-            rows, columns = mx_quantize_both(dy, ctx.fmt)
-        elif ctx.wc is not None:
-            rows = mx_quantize(dy, ctx.fmt)
-        else:
-            columns = mx_quantize_columns(dy, ctx.fmt)
-        if ctx.wc is not None:
-            dx = mx_matmul(rows, ctx.wc, ctx.types[0])
-        if ctx.xc is not None:
-            dw = mx_matmul(columns, ctx.xc, ctx.types[1])
-        return dx, dw, None
-
-
 def _check_weight(x, w):
     if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != x.shape[-1] or w.shape[0] == 0:
         raise ValueError("the weight must be a matrix with one column for each feature of x")
@@ -164,33 +130,15 @@ def _check_weight(x, w):
 
 def mx_linear(x, w, fmt: str = "e4m3"):
     """x @ w.T with both operands quantised, blocks of 32 along the features; the gradients of x and w come from quantised
-    operands too, their blocks along what each product sums over (straight through the rounding).  The result has x's dtype."""
-    _format(fmt)
+    operands too, their blocks along what each product sums over (straight through the rounding): dx = Q(dy) Q(w^T)^T,
+    dw = Q(dy^T) Q(x^T)^T.  Kept for them: x and w by columns, as far as they are wanted.  The result has x's dtype."""
+    code = _format(fmt)
     flat = _matrix(x)
     _check_weight(x, w)
     if flat.shape[0] == 0:
         return flat.new_empty(*x.shape[:-1], w.shape[0]) + 0 * (flat.sum() + w.sum()).to(x.dtype)      # no rows: gradients are 0
-    y = _MxLinear.apply(flat, w, fmt)
+    y = _call("mx_linear", flat, w, code)
     return y if x.dim() == 2 else y.view(*x.shape[:-1], w.shape[0])
-
-
-class _RmsNorm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, residual, w, eps):
-        y, _, h, rstd = _call("rms_norm_forward", x, residual, w, eps, True, -1, True)
-        ctx.fused = residual is not None
-        ctx.save_for_backward(x if h is None else h, w, rstd)
-        ctx.set_materialize_grads(False)
-        return (y, h) if ctx.fused else y
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dy, dh=None):
-        h, w, rstd = ctx.saved_tensors
-        if dy is None:
-            return dh, dh if ctx.fused else None, None, None
-        dx, dw = _call("rms_norm_backward", dy, dh, h, w, rstd, ctx.needs_input_grad[2])
-        return dx, dx if ctx.fused else None, dw, None
 
 
 def _norm_args(x, w, residual):
@@ -202,6 +150,13 @@ def _norm_args(x, w, residual):
     return flat, residual
 
 
+def _shaped(got, x):
+    y, h = got
+    if x.dim() == 2:
+        return y, x if h is None else h
+    return y.view(x.shape), x if h is None else h.view(x.shape)
+
+
 def rms_norm(x, weight, residual=None, eps: float = 1e-6):
     """(y, h): h = x + residual rounded to x's dtype (x itself without a residual), y = h / sqrt(mean(h^2) + eps) * weight over the last
     dimension.  weight: x's dtype or float32.  Differentiable in x, residual and weight."""
@@ -209,10 +164,7 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6):
     if flat.shape[0] == 0:
         h = x if residual is None else x + residual
         return (h * weight).to(x.dtype), h
-    if res is None:
-        return _RmsNorm.apply(flat, None, weight, float(eps)).view(x.shape), x
-    y, h = _RmsNorm.apply(flat, res, weight, float(eps))
-    return y.view(x.shape), h.view(x.shape)
+    return _shaped(_call("rms_norm", flat, res, weight, eps), x)
 
 
 def rms_norm_mx(x, weight, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
@@ -221,51 +173,23 @@ def rms_norm_mx(x, weight, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
     flat, res = _norm_args(x, weight, residual)
     if flat.shape[0] == 0:
         return _empty(flat, fmt), x if residual is None else x + residual
-    _, blob, h, _ = _call("rms_norm_forward", flat, res, weight, float(eps), False, code, False)
+    blob, h = _call("rms_norm_mx", flat, res, weight, eps, code)
     return MxTensor(blob, flat.shape[0], flat.shape[1], fmt), x if h is None else h.view(x.shape)
 
 
-class _MxNormLinear(torch.autograd.Function):
-    """The norm's 8- or 4-bit output goes straight into the product; kept for backward: h and rstd, from which the product's
-    input is made again, and the weight's columns."""
-
-    @staticmethod
-    def forward(ctx, x, residual, g, w, eps, fmt):
-        _, blob, h, rstd = _call("rms_norm_forward", x, residual, g, eps, False, _FORMATS[fmt], True)
-        wr, ctx.wc = mx_quantize_both(w, fmt)
-        out = mx_matmul(MxTensor(blob, x.shape[0], x.shape[1], fmt), wr, x.dtype)
-        ctx.fmt, ctx.eps, ctx.fused, ctx.w_dtype = fmt, eps, residual is not None, w.dtype
-        ctx.save_for_backward(x if h is None else h, g, rstd)
-        ctx.set_materialize_grads(False)
-        return (out, h) if ctx.fused else out
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dout, dh=None):
-        h, g, rstd = ctx.saved_tensors
-        if dout is None:
-            return dh, dh if ctx.fused else None, None, None, None, None
-        rows, columns = mx_quantize_both(dout, ctx.fmt)
-        dw = None
-        if ctx.needs_input_grad[3]:
-            y = _call("rms_norm_forward", h, None, g, ctx.eps, True, -1, False)[0]
-            dw = mx_matmul(columns, mx_quantize_columns(y, ctx.fmt), ctx.w_dtype)
-        dy = mx_matmul(rows, ctx.wc, h.dtype)
-        dx, dg = _call("rms_norm_backward", dy, dh, h, g, rstd, ctx.needs_input_grad[2])
-        return dx, dx if ctx.fused else None, dg, dw, None, None
-
-
 def mx_norm_linear(x, norm_weight, w, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
-    """(mx_linear of the norm, h) with nothing kept of the norm's output: (out, h) as of rms_norm and mx_linear."""
-    _format(fmt)
+    """(out, h): the norm and the linear layer behind it.  The norm's output goes into the product in few bits and is not kept: the
+    backward pass makes it again from h and one number a row.  Gradients as of mx_linear and rms_norm."""
+    code = _format(fmt)
     flat, res = _norm_args(x, norm_weight, residual)
     _check_weight(x, w)
     if flat.shape[0] == 0:
         y, h = rms_norm(x, norm_weight, residual, eps)
         return mx_linear(y, w, fmt), h
-    got = _MxNormLinear.apply(flat, res, norm_weight, w, float(eps), fmt)
-    out, h = got if res is not None else (got, flat)
-    return out.view(*x.shape[:-1], w.shape[0]), h.view(x.shape)
+    out, h = _call("mx_norm_linear", flat, res, norm_weight, w, eps, code)
+    if x.dim() == 2:
+        return out, x if h is None else h
+    return out.view(*x.shape[:-1], w.shape[0]), x if h is None else h.view(x.shape)
 
 
 class TokenLogprobs(NamedTuple):
@@ -273,24 +197,6 @@ class TokenLogprobs(NamedTuple):
     entropy: torch.Tensor
     top_logprobs: torch.Tensor
     top_indices: torch.Tensor
-
-
-class _TokenLogprobs(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, logits, targets, top):
-        logprobs, entropy, stats, top_logprobs, top_indices = _call("token_logprobs_forward", logits, targets, top)
-        ctx.save_for_backward(logits, targets, stats, entropy)
-        ctx.mark_non_differentiable(top_logprobs, top_indices)
-        ctx.set_materialize_grads(False)
-        return logprobs, entropy, top_logprobs, top_indices
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dlogprobs, dentropy, _top, _indices):
-        logits, targets, stats, entropy = ctx.saved_tensors
-        if dlogprobs is None and dentropy is None:
-            return None, None, None
-        return _call("token_logprobs_backward", logits, targets, stats, entropy, dlogprobs, dentropy), None, None
 
 
 def token_logprobs(logits, targets, top: int = 0) -> TokenLogprobs:
@@ -308,7 +214,7 @@ def token_logprobs(logits, targets, top: int = 0) -> TokenLogprobs:
         none = flat.sum(-1).float()
         return TokenLogprobs(none.view(targets.shape), none.clone().view(targets.shape), none.new_empty(*targets.shape, top),
                              targets.new_empty(*targets.shape, top))
-    got = _TokenLogprobs.apply(flat, targets.reshape(-1), top)
+    got = _call("token_logprobs", flat, targets if logits.dim() == 2 else targets.reshape(-1), top)
     if logits.dim() == 2:
         return TokenLogprobs(*got)
     return TokenLogprobs(got[0].view(targets.shape), got[1].view(targets.shape), got[2].view(*targets.shape, top), got[3].view(*targets.shape, top))
