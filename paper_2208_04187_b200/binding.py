@@ -403,6 +403,7 @@ def native():
         loader = importlib.machinery.ExtensionFileLoader("_native", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_native", loader))
         loader.exec_module(module)
+        module.set_error(DivisionError)
         _native = module
     return _native
 

@@ -74,7 +74,7 @@ def _build_native(verbose):
                 sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     _run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC",
           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] + ["-I" + i for i in includes] +
-         [NATIVE_SRC, "-o", NATIVE_PATH, "-L" + os.path.join(root, "lib"), "-L" + PKG_DIR, "-ltorch_python", "-ltorch_cpu", "-lc10",
+         [NATIVE_SRC, "-o", NATIVE_PATH, "-L" + os.path.join(root, "lib"), "-L" + PKG_DIR, "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10",
           "-lc10_cuda", "-l:libdivision.so", "-Wl,-rpath,$ORIGIN"], verbose, None)
 
 

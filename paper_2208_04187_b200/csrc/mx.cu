@@ -211,10 +211,8 @@ div_status quantize_launch(const MxQuantParams& p, bool rows, bool cols, bool ve
         rows ? (cols ? (vec ? mx_quantize_kernel<XT, FMT, true, true, true> : mx_quantize_kernel<XT, FMT, true, true, false>)
                      : (vec ? mx_quantize_kernel<XT, FMT, true, false, true> : mx_quantize_kernel<XT, FMT, true, false, false>))
              : (vec ? mx_quantize_kernel<XT, FMT, false, true, true> : mx_quantize_kernel<XT, FMT, false, true, false>);
-    if (smem > 48u * 1024u && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-        cudaGetLastError();
-        return DIV_ERR_CUDA;
-    }
+    static SmemAllowed allowed[4];
+    if (cols && !allowed[(rows ? 2 : 0) + (vec ? 1 : 0)]((const void*)kern, smem)) return DIV_ERR_CUDA;
     return launch_pdl(kern, dim3(grid), MXQ_THREADS, smem, st, p);
 }
 

@@ -23,6 +23,8 @@
 #include <cuda_fp4.h>
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "../../include/division.h"
 #include "fused.cuh"
 
@@ -172,6 +174,22 @@ __device__ __forceinline__ void store8_any(T* p, uint32_t left, const float (&v)
 inline bool aligned_16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool lm_dtype_ok(int32_t t) { return t == DIV_F32 || t == DIV_BF16 || t == DIV_F16; }
 inline uint32_t lm_dtype_bytes(int32_t t) { return t == DIV_F32 ? 4u : 2u; }
+// a kernel's leave to use more than 48 KB of shared memory, asked for once on each device
+struct SmemAllowed {
+    std::atomic<uint64_t> devices{0};
+    bool operator()(const void* kern, uint32_t bytes) {
+        int device = 0;
+        if (cudaGetDevice(&device) != cudaSuccess) return false;
+        const uint64_t bit = device < 64 ? 1ull << device : 0u;
+        if (devices.load(std::memory_order_acquire) & bit) return true;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+            cudaGetLastError();
+            return false;
+        }
+        devices.fetch_or(bit, std::memory_order_release);
+        return true;
+    }
+};
 inline bool mx_format_ok(int32_t f) { return f == MX_E4M3 || f == MX_E2M1; }
 inline bool lm_size_ok(int64_t v) { return v >= 1 && v < (1ll << 31) - 512; }
 template <typename F>

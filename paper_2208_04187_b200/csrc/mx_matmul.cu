@@ -111,13 +111,16 @@ __device__ __forceinline__ void mxp_load16(uint32_t at, uint32_t (&v)[32]) {
 }
 // waits for a phase, at most MXP_LIMIT_NS, and not once another thread of the CTA has given up
 __device__ __forceinline__ bool mxp_wait(uint64_t* bar, uint32_t parity, MxCtl* ctl) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = now_ns();
+    uint64_t t0 = 0;
     for (uint32_t polls = 1;; ++polls) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((polls & 63u) == 0u && (*(volatile uint32_t*)&ctl->failed || now_ns() - t0 > MXP_LIMIT_NS)) {
-            *(volatile uint32_t*)&ctl->failed = 1u;
-            return false;
+        if ((polls & 63u) == 0u) {                         // (reading the timer takes longer than most waits)
+            const uint64_t t = now_ns();
+            if (t0 == 0u) t0 = t;
+            if (*(volatile uint32_t*)&ctl->failed || t - t0 > MXP_LIMIT_NS) {
+                *(volatile uint32_t*)&ctl->failed = 1u;
+                return false;
+            }
         }
     }
 }
@@ -362,19 +365,193 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
     }
 }
 
+// ---------------------------------------------------------------------------------------------
+// one to four tokens
+// ---------------------------------------------------------------------------------------------
+// A few rows of S against all rows of P are bound by the reading of P, and by launch and latency before that: the tensor cores'
+// tile would be empty but for a few columns, and its way out through a cluster takes as long as everything else.  Here a CTA takes 8
+// rows of P; its 4 warps share the stages, 8 lanes a row's stage, a 16-byte piece each.  All of S lies in shared memory in 16 bits, which
+// hold every code's value.  A block of e2m1 sums exactly in 16 bits (8 products of at most 36, in steps of 1/4, to a half of a register),
+// products of e4m3 go in 32; the block's sum is scaled by both powers of two at once.
+// 4096 x 4096 e2m1, one token: see MXV_MAX_SMEM for where the tensor cores' kernel takes over.
+constexpr uint32_t MXV_THREADS = 128, MXV_ROWS = 8, MXV_MAX_TOKENS = 4;
+constexpr uint32_t MXV_MAX_SMEM = 96u * 1024u;             // of the tokens
+
+__host__ __device__ inline uint32_t mxv_smem(uint32_t tokens, uint32_t stages, int fmt) {
+    return tokens * stages * mx_stage(fmt) * 2u + tokens * stages * (mx_stage(fmt) / 32u);         // values, scale bytes
+}
+// dot * 2^(a - 127) * 2^(b - 127)
+__device__ __forceinline__ float mxv_scaled(float dot, uint32_t a, uint32_t b) {
+    if (a == 255u || b == 255u) return __uint_as_float(0x7FC00000u);
+    const int t = (int)(a + b) - 254, h = t >> 1;                    // halves, both normal powers: no way round beyond the range
+    return dot * __uint_as_float((uint32_t)(h + 127) << 23) * __uint_as_float((uint32_t)(t - h + 127) << 23);
+}
+// 16 bytes of codes as pairs of 16-bit numbers: 8 pairs of e4m3, 16 of e2m1
+template <int FMT>
+__device__ __forceinline__ __half2 mxv_pair(const uint32_t (&w)[4], uint32_t i) {
+    const uint32_t code = FMT == MX_E4M3 ? (w[i >> 1] >> (16u * (i & 1u))) & 0xFFFFu : (w[i >> 2] >> (8u * (i & 3u))) & 0xFFu;
+    return __half2(FMT == MX_E4M3 ? __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)code, __NV_E4M3)
+                                  : __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)code, __NV_E2M1));
+}
+
+template <int FMT, uint32_t M>
+__global__ void __launch_bounds__(MXV_THREADS)
+mx_vector_kernel(const __grid_constant__ MxProductParams p) {
+    typedef MxFormat<FMT> F;
+    constexpr uint32_t PAIRS = FMT == MX_E4M3 ? 8u : 16u, UNITS = PAIRS / 4u;      // of a piece: pairs of numbers, 16-byte units of their 16-bit values
+    constexpr uint32_t BLOCKS = F::STAGE / 32u, SETS = MXV_ROWS / 4u, AHEAD = 4u;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float joined[4][MXV_ROWS][M];
+    const uint32_t stages = p.p.s.stages, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    uint4* values = reinterpret_cast<uint4*>(smem);                                // [token][stage][unit of the piece][piece]: 8 lanes read 128 bytes
+    unsigned char* scales = smem + M * stages * F::STAGE * 2u;                     // [token][stage][block]
+    griddep_wait();
+    griddep_launch();
+
+    const uint32_t r0 = blockIdx.x * MXV_ROWS, piece = lane & 7u;
+    const unsigned char *from[SETS], *scale_of[SETS];
+    uint32_t step[SETS], chunk[SETS];
+    bool there[SETS];
+#pragma unroll
+    for (uint32_t s = 0; s < SETS; ++s) {
+        const uint32_t row = r0 + s * 4u + (lane >> 3), rb = row >> 7, rt = row & 127u;
+        there[s] = row < p.p.s.rows;
+        chunk[s] = piece ^ (rt & 7u);
+        step[s] = there[s] ? mx_tile_rows(p.p.s, rb) * 128u : 0u;
+        from[s] = p.p.codes + (there[s] ? mx_tile_offset(p.p.s, rb, 0) + rt * 128u + piece * 16u : 0u);
+        const uint32_t block = FMT == MX_E4M3 ? chunk[s] >> 1 : chunk[s];
+        scale_of[s] = p.p.scales + (there[s] ? (uint64_t)rb * stages * F::ATOMS * 512u + (block >> 2) * 512u + mx_scale_slot(rt) + (block & 3u) : 0u);
+    }
+    uint4 q[AHEAD][SETS];
+    uint32_t e[AHEAD][SETS];
+    const auto bring = [&](uint32_t k) {
+#pragma unroll
+        for (uint32_t a = 0; a < AHEAD; ++a)
+#pragma unroll
+            for (uint32_t s = 0; s < SETS; ++s)
+                if (k + a * 4u < stages && there[s]) {
+                    q[a][s] = *reinterpret_cast<const uint4*>(from[s] + (uint64_t)(k + a * 4u) * step[s]);
+                    e[a][s] = scale_of[s][(uint64_t)(k + a * 4u) * F::ATOMS * 512u];
+                }
+    };
+    bring(warp);                                             // under way while the tokens are brought
+
+    for (uint32_t job = threadIdx.x; job < M * stages * 8u; job += MXV_THREADS) {
+        const uint32_t c = job & 7u, stage = (job >> 3) % stages, t = (job >> 3) / stages;      // (all tokens lie in the first 128 rows)
+        const uint4 x = *reinterpret_cast<const uint4*>(p.s.codes + mx_tile_offset(p.s.s, 0, stage) + mx_piece(t, c));
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (uint32_t u = 0; u < UNITS; ++u) {
+            __half2 v[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) v[i] = mxv_pair<FMT>(w, u * 4u + i);
+            values[((t * stages + stage) * UNITS + u) * 8u + c] = *reinterpret_cast<const uint4*>(v);
+        }
+        if (c < BLOCKS) scales[(t * stages + stage) * BLOCKS + c] = p.s.scales[((uint64_t)stage * F::ATOMS + (c >> 2)) * 512u + mx_scale_slot(t) + (c & 3u)];
+    }
+    __syncthreads();
+
+    float sum[SETS][M];
+#pragma unroll
+    for (uint32_t s = 0; s < SETS; ++s)
+#pragma unroll
+        for (uint32_t t = 0; t < M; ++t) sum[s][t] = 0.f;
+    for (uint32_t k = warp; k < stages; k += 4u * AHEAD) {
+        if (k != warp) bring(k);
+#pragma unroll
+        for (uint32_t a = 0; a < AHEAD; ++a) {
+            const uint32_t stage = k + a * 4u;
+            if (stage >= stages) break;
+#pragma unroll
+            for (uint32_t s = 0; s < SETS; ++s) {
+                if (!there[s]) continue;
+                const uint32_t w[4] = {q[a][s].x, q[a][s].y, q[a][s].z, q[a][s].w};
+                __half2 mine[PAIRS];
+#pragma unroll
+                for (uint32_t i = 0; i < PAIRS; ++i) mine[i] = mxv_pair<FMT>(w, i);
+                const uint32_t block = FMT == MX_E4M3 ? chunk[s] >> 1 : chunk[s];
+#pragma unroll
+                for (uint32_t t = 0; t < M; ++t) {
+                    float dot;
+                    if (FMT == MX_E2M1) {
+                        __half2 part[2] = {__float2half2_rn(0.f), __float2half2_rn(0.f)};
+#pragma unroll
+                        for (uint32_t u = 0; u < UNITS; ++u) {
+                            const uint4 x = values[((t * stages + stage) * UNITS + u) * 8u + chunk[s]];
+                            const __half2* v = reinterpret_cast<const __half2*>(&x);
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i) part[u >> 1] = __hfma2(mine[u * 4u + i], v[i], part[u >> 1]);
+                        }
+                        const float2 lo = __half22float2(part[0]), hi = __half22float2(part[1 % 2]);
+                        dot = (lo.x + lo.y) + (hi.x + hi.y);
+                    } else {
+                        dot = 0.f;
+#pragma unroll
+                        for (uint32_t u = 0; u < UNITS; ++u) {
+                            const uint4 x = values[((t * stages + stage) * UNITS + u) * 8u + chunk[s]];
+                            const __half2* v = reinterpret_cast<const __half2*>(&x);
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i) {
+                                const float2 m = __half22float2(mine[u * 4u + i]), f = __half22float2(v[i]);
+                                dot = fmaf(m.y, f.y, fmaf(m.x, f.x, dot));
+                            }
+                        }
+                    }
+                    sum[s][t] += mxv_scaled(dot, e[a][s], scales[(t * stages + stage) * BLOCKS + block]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < SETS; ++s)
+#pragma unroll
+        for (uint32_t t = 0; t < M; ++t) {
+            float v = sum[s][t];
+#pragma unroll
+            for (int d = 4; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+            if (piece == 0) joined[warp][s * 4u + (lane >> 3)][t] = v;
+        }
+    __syncthreads();
+    if (threadIdx.x < MXV_ROWS * M) {
+        const uint32_t r = threadIdx.x % MXV_ROWS, t = threadIdx.x / MXV_ROWS;
+        if (r0 + r < p.p.s.rows) {
+            const float v = (joined[0][r][t] + joined[1][r][t]) + (joined[2][r][t] + joined[3][r][t]);
+            const uint64_t at = p.swapped ? t * p.ld + (r0 + r) : (r0 + r) * p.ld + t;
+            if (p.out_dtype == DIV_BF16) static_cast<__nv_bfloat16*>(p.out)[at] = from_f32<__nv_bfloat16>(v);
+            else if (p.out_dtype == DIV_F16) static_cast<__half*>(p.out)[at] = from_f32<__half>(v);
+            else static_cast<float*>(p.out)[at] = v;
+        }
+    }
+}
+
 }  // namespace divk
 
 namespace {
 using namespace divk;
 
+template <int FMT, uint32_t M>
+div_status vector_launch(const MxProductParams& p, cudaStream_t st) {
+    static SmemAllowed allowed;
+    auto kern = mx_vector_kernel<FMT, M>;
+    if (!allowed((const void*)kern, MXV_MAX_SMEM)) return DIV_ERR_CUDA;
+    return launch_pdl(kern, dim3((p.p.s.rows + MXV_ROWS - 1u) / MXV_ROWS), MXV_THREADS, mxv_smem(M, p.p.s.stages, FMT), st, p);
+}
+template <int FMT>
+div_status vector_by_tokens(const MxProductParams& p, cudaStream_t st) {
+    switch (p.s.s.rows) {
+        case 1: return vector_launch<FMT, 1>(p, st);
+        case 2: return vector_launch<FMT, 2>(p, st);
+        case 3: return vector_launch<FMT, 3>(p, st);
+    }
+    return vector_launch<FMT, 4>(p, st);
+}
+
 template <int FMT, uint32_t BN>
 div_status product_launch(const MxProductParams& p, uint32_t grid, cudaStream_t st) {
     typedef MxTile<FMT, BN> T;
     auto kern = mx_product_kernel<FMT, BN>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)T::SMEM) != cudaSuccess) {
-        cudaGetLastError();
-        return DIV_ERR_CUDA;
-    }
+    static SmemAllowed allowed;
+    if (!allowed((const void*)kern, T::SMEM)) return DIV_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(MXP_THREADS);
@@ -435,6 +612,8 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     p.out = out_dev;
     p.ld = (uint64_t)out_row_stride;
     p.out_dtype = (uint32_t)out_dtype;
+    if (p.s.s.rows <= MXV_MAX_TOKENS && mxv_smem(p.s.s.rows, p.s.s.stages, format) <= MXV_MAX_SMEM)
+        return format == MX_E4M3 ? vector_by_tokens<MX_E4M3>(p, (cudaStream_t)cuda_stream) : vector_by_tokens<MX_E2M1>(p, (cudaStream_t)cuda_stream);
     p.vec = aligned_16(out_dev) && (m == 1 || out_row_stride * size % 16 == 0);
     const uint64_t rows_s = p.s.s.rows;
     p.tiles_p = (p.p.s.rows + 127u) / 128u;

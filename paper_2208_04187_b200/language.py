@@ -25,21 +25,13 @@ import torch
 
 from . import binding
 
-_FORMATS = binding.MX_FORMATS
+_native = None
 
 
-def _format(fmt: str) -> int:
-    try:
-        return _FORMATS[fmt]
-    except KeyError:
-        raise ValueError(f"fmt must be one of {tuple(_FORMATS)}, not {fmt!r}") from None
-
-
-def _call(name: str, *args):
-    got = getattr(binding._native or binding.native(), name)(*args)
-    if got.__class__ is int:
-        raise binding.DivisionError(got, "div_" + name)
-    return got
+def _load():
+    global _native
+    _native = binding.native()
+    return _native
 
 
 class MxTensor:
@@ -64,50 +56,29 @@ class MxTensor:
 
     def dequantize(self, dtype=torch.bfloat16):
         """The numbers it stands for (exact in bfloat16 and float32)."""
-        if self.rows == 0:
-            return torch.empty(0, self.cols, dtype=dtype, device=self.blob.device)
-        return _call("mx_dequantize", self.blob, self.rows, self.cols, _FORMATS[self.fmt], dtype)
+        return (_native or _load()).mx_dequantize(self.blob, self.rows, self.cols, self.fmt, dtype)
 
     def __repr__(self):
         return f"MxTensor({self.rows} x {self.cols}, {self.fmt}, {self.blob.device})"
 
 
-def _matrix(x, what="x"):
-    if not isinstance(x, torch.Tensor) or x.dim() < 1:
-        raise ValueError(f"{what} must be a tensor of at least one dimension")
-    if x.shape[-1] == 0:
-        raise ValueError(f"{what} has rows of no numbers")
-    return x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
-
-
-def _empty(x, fmt):
-    return MxTensor(torch.empty(0, dtype=torch.uint8, device=x.device), 0, x.shape[1], fmt)
-
-
 def mx_quantize(x, fmt: str = "e4m3") -> MxTensor:
     """x (leading dimensions folded) quantised by rows: blocks along the last dimension.  No gradient passes."""
-    code, x = _format(fmt), _matrix(x)
-    if x.shape[0] == 0:
-        return _empty(x, fmt)
-    return MxTensor(_call("mx_quantize", x, code, True, False)[0], x.shape[0], x.shape[1], fmt)
+    blob, _, rows, cols = (_native or _load()).mx_quantize(x, fmt, True, False)
+    return MxTensor(blob, rows, cols, fmt)
 
 
 def mx_quantize_both(x, fmt: str = "e4m3"):
     """(x by rows, its transpose by rows) from one reading: what the forward product takes, and what the gradient of the
     weights takes, whose sum runs over the rows of x.  No gradient passes."""
-    code, x = _format(fmt), _matrix(x)
-    if x.shape[0] == 0:
-        raise ValueError("x has no rows")
-    rows, columns = _call("mx_quantize", x, code, True, True)
-    return MxTensor(rows, x.shape[0], x.shape[1], fmt), MxTensor(columns, x.shape[1], x.shape[0], fmt)
+    by_rows, by_columns, rows, cols = (_native or _load()).mx_quantize(x, fmt, True, True)
+    return MxTensor(by_rows, rows, cols, fmt), MxTensor(by_columns, cols, rows, fmt)
 
 
 def mx_quantize_columns(x, fmt: str = "e4m3") -> MxTensor:
     """The transpose of x quantised by rows."""
-    code, x = _format(fmt), _matrix(x)
-    if x.shape[0] == 0:
-        raise ValueError("x has no rows")
-    return MxTensor(_call("mx_quantize", x, code, False, True)[1], x.shape[1], x.shape[0], fmt)
+    _, blob, rows, cols = (_native or _load()).mx_quantize(x, fmt, False, True)
+    return MxTensor(blob, cols, rows, fmt)
 
 
 def mx_matmul(a: MxTensor, b: MxTensor, dtype=torch.bfloat16):
@@ -116,80 +87,32 @@ def mx_matmul(a: MxTensor, b: MxTensor, dtype=torch.bfloat16):
         raise ValueError("mx_matmul takes two MxTensors")
     if a.fmt != b.fmt or a.cols != b.cols:
         raise ValueError(f"operands differ in format or length of rows: {a!r}, {b!r}")
-    if a.rows == 0 or b.rows == 0:
-        return torch.empty(a.rows, b.rows, dtype=dtype, device=a.device)
-    return _call("mx_matmul", a.blob, a.rows, b.blob, b.rows, a.cols, _FORMATS[a.fmt], dtype)
-
-
-def _check_weight(x, w):
-    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != x.shape[-1] or w.shape[0] == 0:
-        raise ValueError("the weight must be a matrix with one column for each feature of x")
-    if w.device != x.device:
-        raise ValueError("x and the weight must be on one device")
+    return (_native or _load()).mx_matmul(a.blob, a.rows, b.blob, b.rows, a.cols, a.fmt, dtype)
 
 
 def mx_linear(x, w, fmt: str = "e4m3"):
     """x @ w.T with both operands quantised, blocks of 32 along the features; the gradients of x and w come from quantised
     operands too, their blocks along what each product sums over (straight through the rounding): dx = Q(dy) Q(w^T)^T,
     dw = Q(dy^T) Q(x^T)^T.  Kept for them: x and w by columns, as far as they are wanted.  The result has x's dtype."""
-    code = _format(fmt)
-    flat = _matrix(x)
-    _check_weight(x, w)
-    if flat.shape[0] == 0:
-        return flat.new_empty(*x.shape[:-1], w.shape[0]) + 0 * (flat.sum() + w.sum()).to(x.dtype)      # no rows: gradients are 0
-    y = _call("mx_linear", flat, w, code)
-    return y if x.dim() == 2 else y.view(*x.shape[:-1], w.shape[0])
-
-
-def _norm_args(x, w, residual):
-    flat = _matrix(x)
-    if residual is not None:
-        if not isinstance(residual, torch.Tensor) or residual.shape != x.shape:
-            raise ValueError("residual must have the shape of x")
-        residual = _matrix(residual, "residual")
-    return flat, residual
-
-
-def _shaped(got, x):
-    y, h = got
-    if x.dim() == 2:
-        return y, x if h is None else h
-    return y.view(x.shape), x if h is None else h.view(x.shape)
+    return (_native or _load()).mx_linear(x, w, fmt)
 
 
 def rms_norm(x, weight, residual=None, eps: float = 1e-6):
     """(y, h): h = x + residual rounded to x's dtype (x itself without a residual), y = h / sqrt(mean(h^2) + eps) * weight over the last
     dimension.  weight: x's dtype or float32.  Differentiable in x, residual and weight."""
-    flat, res = _norm_args(x, weight, residual)
-    if flat.shape[0] == 0:
-        h = x if residual is None else x + residual
-        return (h * weight).to(x.dtype), h
-    return _shaped(_call("rms_norm", flat, res, weight, eps), x)
+    return (_native or _load()).rms_norm(x, residual, weight, eps)
 
 
 def rms_norm_mx(x, weight, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
     """(q, h): as rms_norm, with y handed on as an MxTensor (rows folded), quantised from its 32-bit values.  No gradient passes."""
-    code = _format(fmt)
-    flat, res = _norm_args(x, weight, residual)
-    if flat.shape[0] == 0:
-        return _empty(flat, fmt), x if residual is None else x + residual
-    blob, h = _call("rms_norm_mx", flat, res, weight, eps, code)
-    return MxTensor(blob, flat.shape[0], flat.shape[1], fmt), x if h is None else h.view(x.shape)
+    blob, rows, cols, h = (_native or _load()).rms_norm_mx(x, residual, weight, eps, fmt)
+    return MxTensor(blob, rows, cols, fmt), h
 
 
 def mx_norm_linear(x, norm_weight, w, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
     """(out, h): the norm and the linear layer behind it.  The norm's output goes into the product in few bits and is not kept: the
     backward pass makes it again from h and one number a row.  Gradients as of mx_linear and rms_norm."""
-    code = _format(fmt)
-    flat, res = _norm_args(x, norm_weight, residual)
-    _check_weight(x, w)
-    if flat.shape[0] == 0:
-        y, h = rms_norm(x, norm_weight, residual, eps)
-        return mx_linear(y, w, fmt), h
-    out, h = _call("mx_norm_linear", flat, res, norm_weight, w, eps, code)
-    if x.dim() == 2:
-        return out, x if h is None else h
-    return out.view(*x.shape[:-1], w.shape[0]), x if h is None else h.view(x.shape)
+    return (_native or _load()).mx_norm_linear(x, residual, norm_weight, w, eps, fmt)
 
 
 class TokenLogprobs(NamedTuple):
@@ -204,32 +127,24 @@ def token_logprobs(logits, targets, top: int = 0) -> TokenLogprobs:
     32) most probable tokens with theirs, equal ones by index.  logits: ... x vocabulary.  Results in float32.  The logits are all that
     is kept for the backward pass, beside four numbers a row; log probabilities and entropies are differentiable, the alternatives
     are not."""
-    flat = _matrix(logits, "logits")
-    if not isinstance(targets, torch.Tensor) or targets.shape != logits.shape[:-1]:
-        raise ValueError("targets must have the shape of logits without the last dimension")
-    top = int(top)
-    if flat.shape[0] == 0:
-        if not 0 <= top <= min(32, flat.shape[1]):
-            raise ValueError("top must lie between 0 and 32 and not pass the vocabulary")
-        none = flat.sum(-1).float()
-        return TokenLogprobs(none.view(targets.shape), none.clone().view(targets.shape), none.new_empty(*targets.shape, top),
-                             targets.new_empty(*targets.shape, top))
-    got = _call("token_logprobs", flat, targets if logits.dim() == 2 else targets.reshape(-1), top)
-    if logits.dim() == 2:
-        return TokenLogprobs(*got)
-    return TokenLogprobs(got[0].view(targets.shape), got[1].view(targets.shape), got[2].view(*targets.shape, top), got[3].view(*targets.shape, top))
+    return TokenLogprobs(*(_native or _load()).token_logprobs(logits, targets, top))
 
 
 # ------------------------------------------------------------------------------------------------------------
 # modules
 # ------------------------------------------------------------------------------------------------------------
+def _known(fmt):
+    if fmt not in binding.MX_FORMATS:
+        raise ValueError(f"fmt must be one of {tuple(binding.MX_FORMATS)}, not {fmt!r}")
+    return fmt
+
+
 class DivisionLinear(torch.nn.Linear):
     """nn.Linear whose products take quantised operands; what it keeps of its input has 8 or 4 bits a number."""
 
     def __init__(self, in_features, out_features, bias=True, fmt: str = "e4m3", device=None, dtype=None):
         super().__init__(in_features, out_features, bias, device, dtype)
-        _format(fmt)
-        self.fmt = fmt
+        self.fmt = _known(fmt)
 
     def forward(self, x):
         y = mx_linear(x, self.weight, self.fmt)
@@ -253,11 +168,11 @@ class DivisionNormLinear(torch.nn.Module):
 
     def __init__(self, in_features, out_features, eps: float = 1e-6, fmt: str = "e4m3", device=None, dtype=None):
         super().__init__()
-        _format(fmt)
+        self.fmt = _known(fmt)
         self.norm_weight = torch.nn.Parameter(torch.ones(in_features, device=device, dtype=dtype))
         self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device, dtype=dtype))
         torch.nn.init.kaiming_uniform_(self.weight, a=5 ** 0.5)
-        self.eps, self.fmt = eps, fmt
+        self.eps = eps
 
     def forward(self, x, residual=None):
         out, h = mx_norm_linear(x, self.norm_weight, self.weight, residual, self.eps, self.fmt)
