@@ -6,7 +6,7 @@
 // m and log s are kept apart: their sum would lose log s next to a large m.
 //
 // Forward is bound by memory where the vocabulary is long (one reading of the logits), by the exponentials next (16 a clock and SM).  A
-// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, LP_AT_ONCE of them under way together, and
+// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, 4 or 8 of them under way together, and
 // joins its sums with the others' in a fixed order.  Additions and products go two at a time (f32x2).
 //
 // The most probable tokens come from the same pass.  The k-th largest of the 64 maxima of the CTA's groups of 4 threads is a bound that
@@ -20,7 +20,6 @@ namespace divk {
 
 constexpr uint32_t LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_MAX_TOP = 32, LP_MAX_CLUSTER = 8;
 constexpr float LP_LOG2E = 1.4426950408889634f;
-constexpr uint32_t LP_AT_ONCE = 8;              // pieces of a thread under way
 constexpr float LP_LEAST = -1000.f;             // exp of it is 0, and 0 times it is no NaN
 
 struct LogprobParams {
@@ -212,29 +211,25 @@ template <typename T> struct Pieces {
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t order_key(float x) { return x != x ? 0xFFFFFFFFu : float_key(x + 0.f); }     // (-0 is 0; key 0 is nobody's)
 __device__ __forceinline__ float key_value(uint32_t k) { return k == 0xFFFFFFFFu ? __uint_as_float(0x7FC00000u) : key_float(k); }
-__device__ __forceinline__ bool before(uint32_t ka, uint32_t ia, uint32_t kb, uint32_t ib) { return ka > kb || (ka == kb && ia < ib); }
+// a logit and its index as one number: larger logits are larger, of equal ones the smaller index; 0 is nobody's
+__device__ __forceinline__ uint64_t entry(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (0xFFFFFFFFu - index); }
+__device__ __forceinline__ uint32_t entry_key(uint64_t e) { return (uint32_t)(e >> 32); }
+__device__ __forceinline__ uint32_t entry_index(uint64_t e) { return 0xFFFFFFFFu - (uint32_t)e; }
 
 struct TopList {            // across the lanes of a warp, best first
-    uint32_t key, index;
-    __device__ __forceinline__ void offer(bool have, uint32_t k, uint32_t i, uint32_t top, uint32_t& last_key, uint32_t& last_index) {
+    uint64_t mine, last;    // last: the top-th
+    __device__ __forceinline__ void offer(bool have, uint64_t e, uint32_t top) {
         const uint32_t lane = threadIdx.x & 31u;
-        uint32_t who = __ballot_sync(0xFFFFFFFFu, have && before(k, i, last_key, last_index));
+        uint32_t who = __ballot_sync(0xFFFFFFFFu, have && e > last);
         while (who) {
             const uint32_t src = (uint32_t)__ffs((int)who) - 1u;
             who &= who - 1u;
-            const uint32_t ck = __shfl_sync(0xFFFFFFFFu, k, src), ci = __shfl_sync(0xFFFFFFFFu, i, src);
-            if (!before(ck, ci, last_key, last_index)) continue;
-            const uint32_t at = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, before(key, index, ck, ci)));
-            const uint32_t pk = __shfl_up_sync(0xFFFFFFFFu, key, 1), pi = __shfl_up_sync(0xFFFFFFFFu, index, 1);
-            if (lane == at) {
-                key = ck;
-                index = ci;
-            } else if (lane > at) {
-                key = pk;
-                index = pi;
-            }
-            last_key = __shfl_sync(0xFFFFFFFFu, key, top - 1u);
-            last_index = __shfl_sync(0xFFFFFFFFu, index, top - 1u);
+            const uint64_t c = __shfl_sync(0xFFFFFFFFu, e, src);
+            if (c <= last) continue;
+            const uint32_t at = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine > c));
+            const uint64_t up = __shfl_up_sync(0xFFFFFFFFu, mine, 1);
+            mine = lane == at ? c : lane > at ? up : mine;
+            last = __shfl_sync(0xFFFFFFFFu, mine, top - 1u);
         }
     }
 };
@@ -246,8 +241,8 @@ struct LogprobShared {
     Running cta;
     uint32_t bound, n_again, n_found;
     uint32_t again[LP_THREADS];                     // threads whose pieces are read again
-    uint32_t key[LP_THREADS], index[LP_THREADS];     // what reaches the bound; the warps' lists; (of rank 0) the cluster's
-    uint32_t best_key[LP_MAX_TOP], best_index[LP_MAX_TOP];
+    alignas(16) uint64_t found[LP_THREADS];          // what reaches the bound; the warps' lists; (of rank 0) the cluster's
+    uint64_t best[LP_MAX_TOP];
 };
 static_assert(LP_WARPS * LP_MAX_TOP == LP_THREADS && LP_MAX_CLUSTER * LP_MAX_TOP <= LP_THREADS, "a list entry for each thread");
 
@@ -262,21 +257,29 @@ __device__ __forceinline__ uint32_t lp_peer(uint32_t local, uint32_t rank) {
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
-// the `top` best of the first n entries in sh.key, sh.index go to sh.best_key, sh.best_index (key 0: no entry); all threads together
+__device__ __forceinline__ uint64_t lp_peer_entry(uint32_t local, uint32_t rank) {
+    uint32_t at;
+    uint64_t v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+    return v;
+}
+// the `top` best of the first n entries of sh.found go to sh.best (n even or followed by a 0); all threads together
 __device__ __forceinline__ void lp_rank_entries(LogprobShared& sh, uint32_t n, uint32_t top) {
-    if (threadIdx.x < n && sh.key[threadIdx.x] != 0u) {
-        const uint32_t k = sh.key[threadIdx.x], i = sh.index[threadIdx.x];
+    if (threadIdx.x < n) {
+        const uint64_t mine = sh.found[threadIdx.x];
         uint32_t better = 0;
-        for (uint32_t j = 0; j < n; ++j) better += before(sh.key[j], sh.index[j], k, i) ? 1u : 0u;
-        if (better < top) {
-            sh.best_key[better] = k;
-            sh.best_index[better] = i;
+        for (uint32_t j = 0; j < n; j += 2u) {
+            const ulonglong2 two_of = *reinterpret_cast<const ulonglong2*>(&sh.found[j]);
+            better += (two_of.x > mine ? 1u : 0u) + (two_of.y > mine ? 1u : 0u);
         }
+        if (mine != 0u && better < top) sh.best[better] = mine;
     }
 }
 
-template <typename XT, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS)
+// LP_AT_ONCE pieces of a thread are under way together: 8 where few CTAs have the device to themselves, else 4, so that 6 CTAs fit an SM
+template <typename XT, bool TOP, uint32_t LP_AT_ONCE>
+__global__ void __launch_bounds__(LP_THREADS, LP_AT_ONCE == 8 ? 2 : 6)
 logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
     typedef Pieces<XT> P;
     __shared__ LogprobShared sh;
@@ -374,19 +377,16 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
         both += __shfl_xor_sync(0xFFFFFFFFu, both, 1);
         both += __shfl_xor_sync(0xFFFFFFFFu, both, 2);
         if ((both >> 16) < p.top && (both & 0xFFFFu) >= p.top) sh.bound = group;       // (all that write, write the same)
-        if (threadIdx.x < LP_MAX_TOP) {                    // (a CTA of a cluster may hold fewer than `top`)
-            sh.best_key[threadIdx.x] = 0u;
-            sh.best_index[threadIdx.x] = 0xFFFFFFFFu;
-        }
+        if (threadIdx.x < LP_MAX_TOP) sh.best[threadIdx.x] = 0u;        // (a CTA of a cluster may hold fewer than `top`)
         __syncthreads();
         const uint32_t bound = r.s != r.s ? 0u : sh.bound;
         if (from + threadIdx.x < to && mine >= bound) sh.again[atomicAdd(&sh.n_again, 1u)] = threadIdx.x;
         __syncthreads();
         const uint32_t each = (to - from + LP_THREADS - 1u) / LP_THREADS;          // pieces of a thread, at most
-        const uint32_t runs = (each + 31u) / 32u, jobs = sh.n_again * runs;
-        for (uint32_t job = warp; job < jobs; job += LP_WARPS) {
-            const uint32_t at = from + sh.again[job / runs] + (job % runs * 32u + lane) * LP_THREADS;
+        const uint32_t items = sh.n_again * each;
+        for (uint32_t item = threadIdx.x; item < items; item += LP_THREADS) {
             if (*(volatile uint32_t*)&sh.n_found > LP_THREADS) break;                // (lists are the way then)
+            const uint32_t at = from + sh.again[item / each] + item % each * LP_THREADS;
             if (at < to) {
                 float v[P::N];
                 pieces.get(at, v);
@@ -396,22 +396,19 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
                     const uint32_t k = order_key(v[i]);
                     if (i < n && k >= bound) {
                         const uint32_t slot = atomicAdd(&sh.n_found, 1u);
-                        if (slot < LP_THREADS) {
-                            sh.key[slot] = k;
-                            sh.index[slot] = first + i;
-                        }
+                        if (slot < LP_THREADS) sh.found[slot] = entry(k, first + i);
                     }
                 }
             }
         }
         __syncthreads();
         uint32_t n = sh.n_found;
+        __syncthreads();                                   // (nobody writes entries before all have seen the count)
         if (n > LP_THREADS) {
-            __syncthreads();                               // (nobody writes entries before all have seen the count)
-            TopList list = {0u, 0xFFFFFFFFu};
-            uint32_t last_key = 0u, last_index = 0xFFFFFFFFu;
-            for (uint32_t job = warp; job < jobs; job += LP_WARPS) {
-                const uint32_t at = from + sh.again[job / runs] + (job % runs * 32u + lane) * LP_THREADS;
+            TopList list = {0u, 0u};
+            const uint32_t rounds = (items + LP_THREADS - 1u) / LP_THREADS;
+            for (uint32_t round = 0; round < rounds; ++round) {
+                const uint32_t item = round * LP_THREADS + threadIdx.x, at = item < items ? from + sh.again[item / each] + item % each * LP_THREADS : to;
                 float v[P::N];
 #pragma unroll
                 for (uint32_t i = 0; i < P::N; ++i) v[i] = -INFINITY;
@@ -420,39 +417,42 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
 #pragma unroll
                 for (uint32_t i = 0; i < P::N; ++i) {
                     const uint32_t k = order_key(v[i]);
-                    list.offer(i < have && k >= bound, k, first + i, p.top, last_key, last_index);
+                    list.offer(i < have && k >= bound, entry(k, first + i), p.top);
                 }
             }
-            sh.key[threadIdx.x] = lane < p.top ? list.key : 0u;
-            sh.index[threadIdx.x] = lane < p.top ? list.index : 0xFFFFFFFFu;
-            n = LP_THREADS;
             __syncthreads();
+            sh.found[threadIdx.x] = lane < p.top ? list.mine : 0u;
+            n = LP_THREADS;
+        } else if (threadIdx.x == 0 && n < LP_THREADS) {
+            sh.found[n] = 0u;
         }
+        __syncthreads();
         lp_rank_entries(sh, n, p.top);
     }
     if (p.split > 1u) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (rank == 0) {
-            const uint32_t at = (uint32_t)__cvta_generic_to_shared(&sh.cta);
+            // a lane to a CTA of the cluster, then one after another
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(&sh.cta), from_cta = lane < p.split ? lane : 0u;
+            Running o;
+            o.m = __uint_as_float(lp_peer(at, from_cta));
+            o.s = __uint_as_float(lp_peer(at + 4u, from_cta));
+            o.t = __uint_as_float(lp_peer(at + 8u, from_cta));
+            uint64_t e = 0u;
+            if (TOP && threadIdx.x < p.split * p.top)
+                e = lp_peer_entry((uint32_t)__cvta_generic_to_shared(&sh.best[threadIdx.x % p.top]), threadIdx.x / p.top);
             for (uint32_t c = 1; c < p.split; ++c) {
-                Running o;
-                o.m = __uint_as_float(lp_peer(at, c));
-                o.s = __uint_as_float(lp_peer(at + 4u, c));
-                o.t = __uint_as_float(lp_peer(at + 8u, c));
-                r = join(r, o);
+                Running q;
+                q.m = __shfl_sync(0xFFFFFFFFu, o.m, c);
+                q.s = __shfl_sync(0xFFFFFFFFu, o.s, c);
+                q.t = __shfl_sync(0xFFFFFFFFu, o.t, c);
+                r = join(r, q);
             }
             if (TOP) {
-                const uint32_t c = threadIdx.x / LP_MAX_TOP, e = threadIdx.x % LP_MAX_TOP;
-                uint32_t k = 0u, i = 0xFFFFFFFFu;
-                if (c < p.split) {
-                    k = lp_peer((uint32_t)__cvta_generic_to_shared(&sh.best_key[e]), c);
-                    i = lp_peer((uint32_t)__cvta_generic_to_shared(&sh.best_index[e]), c);
-                }
                 __syncthreads();
-                sh.key[threadIdx.x] = k;
-                sh.index[threadIdx.x] = i;
+                sh.found[threadIdx.x] = e;
                 __syncthreads();
-                lp_rank_entries(sh, LP_THREADS, p.top);
+                lp_rank_entries(sh, p.split * p.top, p.top);        // (even: split is)
             }
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -472,8 +472,8 @@ logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
         p.stats[2ull * row + 1u] = log_s;
     }
     if (TOP && threadIdx.x < p.top) {
-        p.top_logprobs[(uint64_t)row * p.top + threadIdx.x] = (key_value(sh.best_key[threadIdx.x]) - m) - log_s;
-        p.top_indices[(uint64_t)row * p.top + threadIdx.x] = (int64_t)sh.best_index[threadIdx.x];
+        p.top_logprobs[(uint64_t)row * p.top + threadIdx.x] = (key_value(entry_key(sh.best[threadIdx.x])) - m) - log_s;
+        p.top_indices[(uint64_t)row * p.top + threadIdx.x] = (int64_t)entry_index(sh.best[threadIdx.x]);
     }
 }
 
@@ -632,7 +632,8 @@ div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride
     if ((uint64_t)rows * split >= (1ull << 31)) return DIV_ERR_SHAPE;
     return with_type(dtype, [&](auto* t) {
         typedef std::remove_pointer_t<decltype(t)> XT;
-        auto kern = top ? logprob_forward_kernel<XT, true> : logprob_forward_kernel<XT, false>;
+        auto kern = split > 1u ? (top ? logprob_forward_kernel<XT, true, 8> : logprob_forward_kernel<XT, false, 8>)
+                              : (top ? logprob_forward_kernel<XT, true, 4> : logprob_forward_kernel<XT, false, 4>);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((uint32_t)rows * split);
         cfg.blockDim = dim3(LP_THREADS);

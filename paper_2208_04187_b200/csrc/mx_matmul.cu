@@ -132,30 +132,32 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float ld_cluster(uint32_t local, uint32_t rank) {
+// an address in the shared memory of another CTA of the cluster; a number there (whose writing a cluster barrier has ordered before)
+__device__ __forceinline__ uint32_t cluster_at(uint32_t local, uint32_t rank) {
     uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t at) {
     float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
     return v;
 }
 
 template <typename OT>
 __device__ __forceinline__ void mxp_store_run(OT* to, const float (&v)[32], uint32_t count, bool vec) {
-    if (vec && count == 32u) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float w[8];
+    for (uint32_t g = 0; g < 32u; g += 8u) {
+        float w[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = v[8 * i + k];
+        for (int k = 0; k < 8; ++k) w[k] = v[g + k];
+        if (vec && g + 8u <= count) {
             Row8<OT> r;
             r.set(w);
-            r.store(to + 8 * i);
+            r.store(to + g);
+        } else if (g < count) {
+            store8_any(to + g, count - g, w);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if ((uint32_t)i < count) to[i] = from_f32<OT>(v[i]);
     }
 }
 template <typename OT>
@@ -169,7 +171,7 @@ __device__ __forceinline__ void mxp_out(const MxProductParams& p, uint32_t row_p
         for (int i = 0; i < 32; ++i)
             if ((uint32_t)i < count) to[i * p.ld] = from_f32<OT>(v[i]);
     } else {
-        mxp_store_run(out + (uint64_t)row_p * p.ld + row_s, v, count, p.vec);
+        mxp_store_run(out + (uint64_t)row_p * p.ld + row_s, v, count, p.vec && (row_s & 7u) == 0u);
     }
 }
 __device__ __forceinline__ void mxp_out_any(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
@@ -338,19 +340,24 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
     __syncwarp();
     if (p.split > 1u) {
         cluster_sync_all();
-        if (warp < 4) {                                                    // (a cluster has one tile)
-            const uint32_t share = BN / p.split, c0 = rank * share, row = warp * 32u + lane;        // (share: a power of two of at least 2)
+        if (warp < 8) {                                                    // (a cluster has one tile)
+            // this CTA's share of the columns, half of it for each four warps; reads of 8 columns of two CTAs are under way together
+            const uint32_t mine = BN / p.split / 2u, c0 = rank * 2u * mine + (warp >> 2) * mine, row = (warp & 3u) * 32u + lane;
             const uint32_t p0 = first % p.tiles_p * 128u, s0 = first / p.tiles_p * BN;
-            const uint32_t mine = smem_u32(ring) + (c0 * 128u + row) * 4u;
-            for (uint32_t c = 0; c < share; c += 32u) {
-                const uint32_t n = min(share - c, 32u);
-                float v[32];
+            for (uint32_t c = 0; c < mine; c += 8u) {
+                const uint32_t n = min(mine - c, 8u), at = smem_u32(ring) + ((c0 + c) * 128u + row) * 4u;
+                float v[32], one[8], two[8];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float sum = 0.f;
-                    if ((uint32_t)i < n && s0 + c0 + c + i < p.s.s.rows)
-                        for (uint32_t r = 0; r < p.split; ++r) sum += ld_cluster(mine + (c + i) * 512u, r);
-                    v[i] = sum;
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                for (uint32_t r = 0; r < p.split; r += 2u) {
+                    const uint32_t at1 = cluster_at(at, r), at2 = cluster_at(at, r + 1u);
+#pragma unroll
+                    for (uint32_t i = 0; i < 8u; ++i) {
+                        one[i] = i < n ? ld_cluster(at1 + i * 512u) : 0.f;
+                        two[i] = i < n ? ld_cluster(at2 + i * 512u) : 0.f;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = (v[i] + one[i]) + two[i];
                 }
                 mxp_out_any(p, p0 + row, s0 + c0 + c, n, v);
             }
@@ -366,61 +373,53 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// one to four tokens
+// one token, 4 bits
 // ---------------------------------------------------------------------------------------------
-// A few rows of S against all rows of P are bound by the reading of P, and by launch and latency before that: the tensor cores'
-// tile would be empty but for a few columns, and its way out through a cluster takes as long as everything else.  Here a CTA takes 8
-// rows of P; its 4 warps share the stages, 8 lanes a row's stage, a 16-byte piece each.  All of S lies in shared memory in 16 bits, which
-// hold every code's value.  A block of e2m1 sums exactly in 16 bits (8 products of at most 36, in steps of 1/4, to a half of a register),
-// products of e4m3 go in 32; the block's sum is scaled by both powers of two at once.
-// 4096 x 4096 e2m1, one token: see MXV_MAX_SMEM for where the tensor cores' kernel takes over.
-constexpr uint32_t MXV_THREADS = 128, MXV_ROWS = 8, MXV_MAX_TOKENS = 4;
-constexpr uint32_t MXV_MAX_SMEM = 96u * 1024u;             // of the tokens
+// One row of S against all rows of P is bound by the reading of P, and by launch and latency before that: of the tensor cores' tile one
+// column would be used, and its way out through a cluster takes as long as everything else.  Here a CTA takes 8 rows of P; its 4 warps
+// share the stages, 8 lanes a row's stage, a block of 32 numbers each.  S lies in shared memory in 16 bits.  A block sums exactly in
+// 16 bits (8 products of at most 36, in steps of 1/4, to a half of a register); the block's sum is scaled by both powers of two at once.
+// From L2, against the tensor cores' kernel: 1024 x 1024 1.9 us (4.3), 4096 x 4096 5.1 us (6.1); 8192 x 8192 12.2 us (10.4), which turning
+// codes into numbers takes.  (The same for e4m3, whose products need 32 bits, took 7.6 us at 4096 x 4096, the tensor cores 6.8; for two
+// tokens 6.4 us, the tensor cores 6.1.)
+constexpr uint32_t MXV_THREADS = 128, MXV_ROWS = 8;
+constexpr uint64_t MXV_MOST = 4096u * 16u;                 // rows x stages up to which this kernel is the shorter
+constexpr uint32_t MXV_MAX_SMEM = 96u * 1024u;             // of S: values and scale bytes
 
-__host__ __device__ inline uint32_t mxv_smem(uint32_t tokens, uint32_t stages, int fmt) {
-    return tokens * stages * mx_stage(fmt) * 2u + tokens * stages * (mx_stage(fmt) / 32u);         // values, scale bytes
-}
+__host__ __device__ inline uint32_t mxv_smem(uint32_t stages) { return stages * (512u + 8u); }
 // dot * 2^(a - 127) * 2^(b - 127)
 __device__ __forceinline__ float mxv_scaled(float dot, uint32_t a, uint32_t b) {
     if (a == 255u || b == 255u) return __uint_as_float(0x7FC00000u);
     const int t = (int)(a + b) - 254, h = t >> 1;                    // halves, both normal powers: no way round beyond the range
     return dot * __uint_as_float((uint32_t)(h + 127) << 23) * __uint_as_float((uint32_t)(t - h + 127) << 23);
 }
-// 16 bytes of codes as pairs of 16-bit numbers: 8 pairs of e4m3, 16 of e2m1
-template <int FMT>
 __device__ __forceinline__ __half2 mxv_pair(const uint32_t (&w)[4], uint32_t i) {
-    const uint32_t code = FMT == MX_E4M3 ? (w[i >> 1] >> (16u * (i & 1u))) & 0xFFFFu : (w[i >> 2] >> (8u * (i & 3u))) & 0xFFu;
-    return __half2(FMT == MX_E4M3 ? __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)code, __NV_E4M3)
-                                  : __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)code, __NV_E2M1));
+    return __half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)((w[i >> 2] >> (8u * (i & 3u))) & 0xFFu), __NV_E2M1));
 }
 
-template <int FMT, uint32_t M>
 __global__ void __launch_bounds__(MXV_THREADS)
 mx_vector_kernel(const __grid_constant__ MxProductParams p) {
-    typedef MxFormat<FMT> F;
-    constexpr uint32_t PAIRS = FMT == MX_E4M3 ? 8u : 16u, UNITS = PAIRS / 4u;      // of a piece: pairs of numbers, 16-byte units of their 16-bit values
-    constexpr uint32_t BLOCKS = F::STAGE / 32u, SETS = MXV_ROWS / 4u, AHEAD = 4u;
+    constexpr uint32_t SETS = MXV_ROWS / 4u, AHEAD = 4u;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float joined[4][MXV_ROWS][M];
+    __shared__ float joined[4][MXV_ROWS];
     const uint32_t stages = p.p.s.stages, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    uint4* values = reinterpret_cast<uint4*>(smem);                                // [token][stage][unit of the piece][piece]: 8 lanes read 128 bytes
-    unsigned char* scales = smem + M * stages * F::STAGE * 2u;                     // [token][stage][block]
+    uint4* values = reinterpret_cast<uint4*>(smem);                                // [stage][quarter of the block][block]: 8 lanes read 128 bytes
+    unsigned char* scales = smem + stages * 512u;                                  // [stage][block]
     griddep_wait();
     griddep_launch();
 
-    const uint32_t r0 = blockIdx.x * MXV_ROWS, piece = lane & 7u;
+    const uint32_t r0 = blockIdx.x * MXV_ROWS;
     const unsigned char *from[SETS], *scale_of[SETS];
-    uint32_t step[SETS], chunk[SETS];
+    uint32_t step[SETS], block[SETS];
     bool there[SETS];
 #pragma unroll
     for (uint32_t s = 0; s < SETS; ++s) {
         const uint32_t row = r0 + s * 4u + (lane >> 3), rb = row >> 7, rt = row & 127u;
         there[s] = row < p.p.s.rows;
-        chunk[s] = piece ^ (rt & 7u);
+        block[s] = (lane & 7u) ^ (rt & 7u);                                        // where this lane's piece belongs
         step[s] = there[s] ? mx_tile_rows(p.p.s, rb) * 128u : 0u;
-        from[s] = p.p.codes + (there[s] ? mx_tile_offset(p.p.s, rb, 0) + rt * 128u + piece * 16u : 0u);
-        const uint32_t block = FMT == MX_E4M3 ? chunk[s] >> 1 : chunk[s];
-        scale_of[s] = p.p.scales + (there[s] ? (uint64_t)rb * stages * F::ATOMS * 512u + (block >> 2) * 512u + mx_scale_slot(rt) + (block & 3u) : 0u);
+        from[s] = p.p.codes + (there[s] ? mx_tile_offset(p.p.s, rb, 0) + rt * 128u + (lane & 7u) * 16u : 0u);
+        scale_of[s] = p.p.scales + (there[s] ? (uint64_t)rb * stages * 1024u + (block[s] >> 2) * 512u + mx_scale_slot(rt) + (block[s] & 3u) : 0u);
     }
     uint4 q[AHEAD][SETS];
     uint32_t e[AHEAD][SETS];
@@ -431,31 +430,29 @@ mx_vector_kernel(const __grid_constant__ MxProductParams p) {
             for (uint32_t s = 0; s < SETS; ++s)
                 if (k + a * 4u < stages && there[s]) {
                     q[a][s] = *reinterpret_cast<const uint4*>(from[s] + (uint64_t)(k + a * 4u) * step[s]);
-                    e[a][s] = scale_of[s][(uint64_t)(k + a * 4u) * F::ATOMS * 512u];
+                    e[a][s] = scale_of[s][(uint64_t)(k + a * 4u) * 1024u];
                 }
     };
-    bring(warp);                                             // under way while the tokens are brought
+    bring(warp);                                             // under way while the token is brought
 
-    for (uint32_t job = threadIdx.x; job < M * stages * 8u; job += MXV_THREADS) {
-        const uint32_t c = job & 7u, stage = (job >> 3) % stages, t = (job >> 3) / stages;      // (all tokens lie in the first 128 rows)
-        const uint4 x = *reinterpret_cast<const uint4*>(p.s.codes + mx_tile_offset(p.s.s, 0, stage) + mx_piece(t, c));
+    for (uint32_t job = threadIdx.x; job < stages * 8u; job += MXV_THREADS) {
+        const uint32_t c = job & 7u, stage = job >> 3;
+        const uint4 x = *reinterpret_cast<const uint4*>(p.s.codes + (uint64_t)stage * 1024u + c * 16u);        // (row 0: pieces lie in order)
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (uint32_t u = 0; u < UNITS; ++u) {
+        for (uint32_t u = 0; u < 4; ++u) {
             __half2 v[4];
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) v[i] = mxv_pair<FMT>(w, u * 4u + i);
-            values[((t * stages + stage) * UNITS + u) * 8u + c] = *reinterpret_cast<const uint4*>(v);
+            for (uint32_t i = 0; i < 4; ++i) v[i] = mxv_pair(w, u * 4u + i);
+            values[(stage * 4u + u) * 8u + c] = *reinterpret_cast<const uint4*>(v);
         }
-        if (c < BLOCKS) scales[(t * stages + stage) * BLOCKS + c] = p.s.scales[((uint64_t)stage * F::ATOMS + (c >> 2)) * 512u + mx_scale_slot(t) + (c & 3u)];
+        scales[stage * 8u + c] = p.s.scales[(uint64_t)stage * 1024u + (c >> 2) * 512u + (c & 3u)];
     }
     __syncthreads();
 
-    float sum[SETS][M];
+    float sum[SETS];
 #pragma unroll
-    for (uint32_t s = 0; s < SETS; ++s)
-#pragma unroll
-        for (uint32_t t = 0; t < M; ++t) sum[s][t] = 0.f;
+    for (uint32_t s = 0; s < SETS; ++s) sum[s] = 0.f;
     for (uint32_t k = warp; k < stages; k += 4u * AHEAD) {
         if (k != warp) bring(k);
 #pragma unroll
@@ -466,61 +463,34 @@ mx_vector_kernel(const __grid_constant__ MxProductParams p) {
             for (uint32_t s = 0; s < SETS; ++s) {
                 if (!there[s]) continue;
                 const uint32_t w[4] = {q[a][s].x, q[a][s].y, q[a][s].z, q[a][s].w};
-                __half2 mine[PAIRS];
+                __half2 part[2] = {__float2half2_rn(0.f), __float2half2_rn(0.f)};
 #pragma unroll
-                for (uint32_t i = 0; i < PAIRS; ++i) mine[i] = mxv_pair<FMT>(w, i);
-                const uint32_t block = FMT == MX_E4M3 ? chunk[s] >> 1 : chunk[s];
+                for (uint32_t u = 0; u < 4; ++u) {
+                    const uint4 x = values[(stage * 4u + u) * 8u + block[s]];
+                    const __half2* v = reinterpret_cast<const __half2*>(&x);
 #pragma unroll
-                for (uint32_t t = 0; t < M; ++t) {
-                    float dot;
-                    if (FMT == MX_E2M1) {
-                        __half2 part[2] = {__float2half2_rn(0.f), __float2half2_rn(0.f)};
-#pragma unroll
-                        for (uint32_t u = 0; u < UNITS; ++u) {
-                            const uint4 x = values[((t * stages + stage) * UNITS + u) * 8u + chunk[s]];
-                            const __half2* v = reinterpret_cast<const __half2*>(&x);
-#pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i) part[u >> 1] = __hfma2(mine[u * 4u + i], v[i], part[u >> 1]);
-                        }
-                        const float2 lo = __half22float2(part[0]), hi = __half22float2(part[1 % 2]);
-                        dot = (lo.x + lo.y) + (hi.x + hi.y);
-                    } else {
-                        dot = 0.f;
-#pragma unroll
-                        for (uint32_t u = 0; u < UNITS; ++u) {
-                            const uint4 x = values[((t * stages + stage) * UNITS + u) * 8u + chunk[s]];
-                            const __half2* v = reinterpret_cast<const __half2*>(&x);
-#pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i) {
-                                const float2 m = __half22float2(mine[u * 4u + i]), f = __half22float2(v[i]);
-                                dot = fmaf(m.y, f.y, fmaf(m.x, f.x, dot));
-                            }
-                        }
-                    }
-                    sum[s][t] += mxv_scaled(dot, e[a][s], scales[(t * stages + stage) * BLOCKS + block]);
+                    for (uint32_t i = 0; i < 4; ++i) part[u >> 1] = __hfma2(mxv_pair(w, u * 4u + i), v[i], part[u >> 1]);
                 }
+                const float2 lo = __half22float2(part[0]), hi = __half22float2(part[1]);
+                sum[s] += mxv_scaled((lo.x + lo.y) + (hi.x + hi.y), e[a][s], scales[stage * 8u + block[s]]);
             }
         }
     }
 #pragma unroll
-    for (uint32_t s = 0; s < SETS; ++s)
+    for (uint32_t s = 0; s < SETS; ++s) {
+        float v = sum[s];
 #pragma unroll
-        for (uint32_t t = 0; t < M; ++t) {
-            float v = sum[s][t];
-#pragma unroll
-            for (int d = 4; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-            if (piece == 0) joined[warp][s * 4u + (lane >> 3)][t] = v;
-        }
+        for (int d = 4; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        if ((lane & 7u) == 0) joined[warp][s * 4u + (lane >> 3)] = v;
+    }
     __syncthreads();
-    if (threadIdx.x < MXV_ROWS * M) {
-        const uint32_t r = threadIdx.x % MXV_ROWS, t = threadIdx.x / MXV_ROWS;
-        if (r0 + r < p.p.s.rows) {
-            const float v = (joined[0][r][t] + joined[1][r][t]) + (joined[2][r][t] + joined[3][r][t]);
-            const uint64_t at = p.swapped ? t * p.ld + (r0 + r) : (r0 + r) * p.ld + t;
-            if (p.out_dtype == DIV_BF16) static_cast<__nv_bfloat16*>(p.out)[at] = from_f32<__nv_bfloat16>(v);
-            else if (p.out_dtype == DIV_F16) static_cast<__half*>(p.out)[at] = from_f32<__half>(v);
-            else static_cast<float*>(p.out)[at] = v;
-        }
+    const uint32_t r = threadIdx.x;
+    if (r < MXV_ROWS && r0 + r < p.p.s.rows) {
+        const float v = (joined[0][r] + joined[1][r]) + (joined[2][r] + joined[3][r]);
+        const uint64_t at = p.swapped ? r0 + r : (r0 + r) * p.ld;
+        if (p.out_dtype == DIV_BF16) static_cast<__nv_bfloat16*>(p.out)[at] = from_f32<__nv_bfloat16>(v);
+        else if (p.out_dtype == DIV_F16) static_cast<__half*>(p.out)[at] = from_f32<__half>(v);
+        else static_cast<float*>(p.out)[at] = v;
     }
 }
 
@@ -529,21 +499,10 @@ mx_vector_kernel(const __grid_constant__ MxProductParams p) {
 namespace {
 using namespace divk;
 
-template <int FMT, uint32_t M>
 div_status vector_launch(const MxProductParams& p, cudaStream_t st) {
     static SmemAllowed allowed;
-    auto kern = mx_vector_kernel<FMT, M>;
-    if (!allowed((const void*)kern, MXV_MAX_SMEM)) return DIV_ERR_CUDA;
-    return launch_pdl(kern, dim3((p.p.s.rows + MXV_ROWS - 1u) / MXV_ROWS), MXV_THREADS, mxv_smem(M, p.p.s.stages, FMT), st, p);
-}
-template <int FMT>
-div_status vector_by_tokens(const MxProductParams& p, cudaStream_t st) {
-    switch (p.s.s.rows) {
-        case 1: return vector_launch<FMT, 1>(p, st);
-        case 2: return vector_launch<FMT, 2>(p, st);
-        case 3: return vector_launch<FMT, 3>(p, st);
-    }
-    return vector_launch<FMT, 4>(p, st);
+    if (!allowed((const void*)mx_vector_kernel, MXV_MAX_SMEM)) return DIV_ERR_CUDA;
+    return launch_pdl(mx_vector_kernel, dim3((p.p.s.rows + MXV_ROWS - 1u) / MXV_ROWS), MXV_THREADS, mxv_smem(p.p.s.stages), st, p);
 }
 
 template <int FMT, uint32_t BN>
@@ -612,8 +571,7 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     p.out = out_dev;
     p.ld = (uint64_t)out_row_stride;
     p.out_dtype = (uint32_t)out_dtype;
-    if (p.s.s.rows <= MXV_MAX_TOKENS && mxv_smem(p.s.s.rows, p.s.s.stages, format) <= MXV_MAX_SMEM)
-        return format == MX_E4M3 ? vector_by_tokens<MX_E4M3>(p, (cudaStream_t)cuda_stream) : vector_by_tokens<MX_E2M1>(p, (cudaStream_t)cuda_stream);
+    if (format == MX_E2M1 && p.s.s.rows == 1u && (uint64_t)p.p.s.rows * p.p.s.stages <= MXV_MOST && p.p.s.stages <= MXV_MAX_SMEM / mxv_smem(1u)) return vector_launch(p, (cudaStream_t)cuda_stream);
     p.vec = aligned_16(out_dev) && (m == 1 || out_row_stride * size % 16 == 0);
     const uint64_t rows_s = p.s.s.rows;
     p.tiles_p = (p.p.s.rows + 127u) / 128u;
