@@ -30,7 +30,7 @@ struct NormParams {
     uint32_t group;            // threads of a row
 };
 
-// sum over the `group` threads of a row (a power of two of at least 32; all threads of the CTA come here together)
+// sum over the `group` threads of a row (whole warps, all of the CTA's or a power of two that divides them; all threads come here together)
 __device__ __forceinline__ float norm_sum(float v, uint32_t group, float* shared) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
@@ -52,6 +52,16 @@ __device__ __forceinline__ void norm_load(const T* p, uint32_t left, float (&v)[
         r.get(v);
     } else {
         load8_any(p, left, v);
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void norm_raw(const T* p, uint32_t left, Row8<T>& r) {
+    if (VEC) {
+        r.load(p);
+    } else {
+        float v[8];
+        load8_any(p, left, v);
+        r.set(v);                       // (exact: they come from T)
     }
 }
 template <typename T, bool VEC>
@@ -199,30 +209,40 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
         for (int j = 0; j < HELD; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[j][i] = 0.f;
-        for (uint32_t k = 0; k < rounds; ++k) {
-            const uint64_t wide = (uint64_t)k * step + mine;
-            const bool there = wide < p.rows;
-            const uint64_t row = there ? wide : 0u;
-            const float rstd = there ? p.rstd[row] : 0.f;
-            float g[N][8], n[N][8], add[N][8];
-            float dot = 0.f;
+        // the next row's dy and h are under way while this one is summed and written
+        Row8<XT> dy[N], h[N], dh[N];
+        float rstd = 0.f, next_rstd = 0.f;
+        const auto bring = [&](uint32_t k) {
+            const uint64_t row = (uint64_t)k * step + mine;
+            const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            next_rstd = row < p.rows ? p.rstd[row] : 0.f;
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
                 const uint32_t at = j * p.group + t;
-                const bool in = there && at * 8u < p.cols;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) g[j][i] = n[j][i] = add[j][i] = 0.f;
-                if (in) {
-                    norm_load<XT, VEC>(static_cast<const XT*>(p.dy) + row * p.dy_stride + at * 8u, p.cols - at * 8u, g[j]);
-                    norm_load<XT, VEC>(static_cast<const XT*>(p.h) + row * p.h_stride + at * 8u, p.cols - at * 8u, n[j]);
-                    if (p.dh) norm_load<XT, VEC>(static_cast<const XT*>(p.dh) + row * p.dh_stride + at * 8u, p.cols - at * 8u, add[j]);
+                dy[j].set(zero);
+                h[j].set(zero);
+                if (row < p.rows && at * 8u < p.cols) {
+                    norm_raw<XT, VEC>(static_cast<const XT*>(p.dy) + row * p.dy_stride + at * 8u, p.cols - at * 8u, dy[j]);
+                    norm_raw<XT, VEC>(static_cast<const XT*>(p.h) + row * p.h_stride + at * 8u, p.cols - at * 8u, h[j]);
                 }
             }
+        };
+        bring(0);
+        for (uint32_t k = 0; k < rounds; ++k) {
+            const uint64_t row = (uint64_t)k * step + mine;
+            const bool there = row < p.rows;
+            float g[N][8], n[N][8];
+            float dot = 0.f;
+            rstd = next_rstd;
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
                 const uint32_t at = j * p.group + t;
+                if (p.dh && there && at * 8u < p.cols)
+                    norm_raw<XT, VEC>(static_cast<const XT*>(p.dh) + row * p.dh_stride + at * 8u, p.cols - at * 8u, dh[j]);
                 float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                 if (at * 8u < p.cols) norm_load<WT, VEC>(static_cast<const WT*>(p.w) + at * 8u, p.cols - at * 8u, w);
+                dy[j].get(g[j]);
+                h[j].get(n[j]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     n[j][i] *= rstd;
@@ -231,14 +251,16 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
                     dot = fmaf(g[j][i], n[j][i], dot);
                 }
             }
+            bring(k + 1u);
             const float mean = norm_sum(dot, p.group, shared) * inv;
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
                 const uint32_t at = j * p.group + t;
                 if (there && at * 8u < p.cols) {
-                    float d[8];
+                    float d[8], add[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    if (p.dh) dh[j].get(add);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, fmaf(-n[j][i], mean, g[j][i]), add[j][i]);
+                    for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, fmaf(-n[j][i], mean, g[j][i]), add[i]);
                     norm_store<XT, VEC>(static_cast<XT*>(p.dx) + row * p.cols + at * 8u, p.cols - at * 8u, d);
                 }
             }
@@ -332,7 +354,9 @@ NormSplit norm_split(uint64_t pieces, uint64_t rows) {
     if (pieces > NORM_MAX_HELD / 8u) return {NORM_MAX_THREADS, 0u, NORM_MAX_THREADS};
     // two pieces a thread once rows fill the device, or where one would take more threads than there are
     s.held = pieces > 2u * NORM_MAX_THREADS ? 4u : pieces > NORM_MAX_THREADS || (rows >= 1024u && pieces >= 64u) ? 2u : 1u;
-    s.group = pow2_up((uint32_t)((pieces + s.held - 1u) / s.held));
+    const uint32_t need = (uint32_t)((pieces + s.held - 1u) / s.held);
+    // rows of up to 128 threads share a CTA of 128; longer ones have a CTA of whole warps
+    s.group = need <= 128u ? pow2_up(need) : (need + 31u) / 32u * 32u;
     s.threads = s.group < 128u ? 128u : s.group;
     return s;
 }
