@@ -47,18 +47,20 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
     griddep_launch();
 
     Row8<XT> raw[8];
-    const XT* x = static_cast<const XT*>(p.x);
+    const Rows<XT> x(p.x, p.r.rows, p.r.cols, p.stride);
+    constexpr int AT_ONCE = VEC || sizeof(XT) == 2 ? 8 : 4;                    // (what lies unaligned takes more registers on its way)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t r = r0 + row_in + 16u * i;
-        const bool there = r < p.r.rows && left != 0u;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (VEC) {
-            if (there) raw[i].load(x + (uint64_t)r * p.stride + c);
-            else raw[i].set(v);
-        } else {
-            if (there) load8_any(x + (uint64_t)r * p.stride + c, left, v);
-            raw[i].set(v);                                                     // (exact: they come from XT)
+    for (int i0 = 0; i0 < 8; i0 += AT_ONCE) {
+        Asked8<XT, VEC> a[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const uint32_t r = r0 + row_in + 16u * (i0 + i);
+            a[i].ask(x, r, c / 8u, r < p.r.rows ? left : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const uint32_t r = r0 + row_in + 16u * (i0 + i);
+            a[i].take(x, r, c / 8u, r < p.r.rows ? left : 0u, raw[i0 + i]);
         }
     }
     if (COLS) {
@@ -73,9 +75,7 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
             const uint32_t rt = row_in + 16u * i;
             float v[8];
             raw[i].get(v);
-            uint32_t big = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) big = max(big, magnitude(v[k]));
+            uint32_t big = raw[i].largest();
             big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
             big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
             const uint32_t e = mx_scale_byte<FMT>(big);
@@ -109,22 +109,25 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
             const XT* from = numbers + block * 32u * MXQ_TILE + col;
 #pragma unroll
             for (int i = 0; i < 32; ++i) word[i] = *reinterpret_cast<const uint32_t*>(from + i * MXQ_TILE);
+            uint32_t big_of_each = word[0];                        // of the column, or of the two
+            if constexpr (W == 2) {
+#pragma unroll
+                for (int i = 1; i < 32; ++i) big_of_each = larger_of_each<XT>(big_of_each, word[i]);
+            }
 #pragma unroll
             for (uint32_t w = 0; w < W; ++w) {
                 float v[4][8];
                 uint32_t big = 0;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    float f;
-                    if (W == 1) {
-                        f = __uint_as_float(word[i]);
+                    if constexpr (W == 1) {
+                        v[i >> 3][i & 7] = __uint_as_float(word[i]);
+                        big = max(big, word[i] & 0x7FFFFFFFu);
                     } else {
-                        const unsigned short h = (unsigned short)(word[i] >> (16u * w));
-                        f = to_f32(*reinterpret_cast<const XT*>(&h));
+                        v[i >> 3][i & 7] = half_of<XT>(word[i], w);
                     }
-                    v[i >> 3][i & 7] = f;
-                    big = max(big, magnitude(f));
                 }
+                if constexpr (W == 2) big = magnitude(half_of<XT>(big_of_each, w));
                 const uint32_t e = mx_scale_byte<FMT>(big);
                 const float inverse = mx_inverse(e);
                 const uint32_t row = col + w;
@@ -168,13 +171,20 @@ mx_dequantize_kernel(const unsigned char* blob, MxShape s, OT* out) {
     const uint32_t rt = (uint32_t)line & 127u, rb = (uint32_t)(tile / s.stages), stage = (uint32_t)(tile % s.stages);
     const uint64_t row = (uint64_t)rb * 128u + rt;
     const uint32_t c = stage * F::STAGE + piece * PER;
-    if (row >= s.rows || c >= s.cols) return;
-    const uint4 q = *reinterpret_cast<const uint4*>(blob + mx_tile_offset(s, rb, stage) + mx_piece(rt, piece));
-    const uint32_t block = piece * PER / 32u;                     // of the stage
-    const uint32_t e = blob[mx_scales_at(s) + ((uint64_t)tile * F::ATOMS + block / 4u) * 512u + mx_scale_slot(rt) + (block & 3u)];
+    const uint32_t left = row < s.rows && c < s.cols ? s.cols - c : 0u;
+    if (VEC && left == 0u) return;
+    uint4 q = make_uint4(0u, 0u, 0u, 0u);
+    uint32_t e = 0;
+    if (left) {
+        q = *reinterpret_cast<const uint4*>(blob + mx_tile_offset(s, rb, stage) + mx_piece(rt, piece));
+        const uint32_t block = piece * PER / 32u;                 // of the stage
+        e = blob[mx_scales_at(s) + ((uint64_t)tile * F::ATOMS + block / 4u) * 512u + mx_scale_slot(rt) + (block & 3u)];
+    }
     const float scale = mx_scale(e);
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    OT* to = out + row * s.cols + c;
+    OT* to = out + (left ? row * s.cols + c : 0u);
+    constexpr int N = Raw8<OT>::N;                                // 16-byte units of 8 numbers
+    uint4 units[PER / 8u * N];
 #pragma unroll
     for (uint32_t h = 0; h < PER / 8u; ++h) {
         float v[8];
@@ -187,15 +197,19 @@ mx_dequantize_kernel(const unsigned char* blob, MxShape s, OT* out) {
             v[2 * i] = __fmul_rn(f.x, scale);
             v[2 * i + 1] = __fmul_rn(f.y, scale);
         }
-        if (VEC) {
-            if (c + h * 8u < s.cols) {
-                Row8<OT> r;
-                r.set(v);
-                r.store(to + h * 8u);
-            }
-        } else if (c + h * 8u < s.cols) {
-            store8_any(to + h * 8u, s.cols - c - h * 8u, v);
-        }
+        Row8<OT> r;
+        r.set(v);
+        uint4 some[N];
+        to_units(r, some);
+#pragma unroll
+        for (int u = 0; u < N; ++u) units[h * N + u] = some[u];
+    }
+    if (VEC) {
+#pragma unroll
+        for (uint32_t u = 0; u < PER / 8u * N; ++u)
+            if (u / N * 8u < left) reinterpret_cast<uint4*>(to)[u] = units[u];
+    } else {
+        Units<OT>::store(to, left, units, piece == 0u, piece == 7u);
     }
 }
 

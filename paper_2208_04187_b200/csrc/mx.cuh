@@ -5,7 +5,7 @@
 //
 //   scale   the smallest power of two with which the block's largest magnitude does not pass the largest number of the
 //           format (448 or 6), between 2^-127 and 2^127: nothing is clipped.  A block that holds an infinity or a NaN has
-//           the scale byte 255, which stands for NaN, and codes 0.
+//           the scale byte 255, which stands for NaN, and any codes.
 //   code    value / scale, rounded to nearest, ties to even.  The division is a product with a power of two, so that it is
 //           exact but for what lies far below the smallest code: quantising rounds once.
 //
@@ -73,8 +73,8 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest) {
     const int s = FMT == MX_E4M3 ? e - 8 + (f > 0x600000) : e - 2 + (f > 0x400000);
     return s < 0 ? 0u : (uint32_t)s;
 }
-__device__ __forceinline__ float mx_inverse(uint32_t scale_byte) {       // 1 / scale, a normal number for 0..253; 0 for NaN blocks
-    return scale_byte == 255u ? 0.f : __uint_as_float((254u - scale_byte) << 23);
+__device__ __forceinline__ float mx_inverse(uint32_t scale_byte) {       // 1 / scale, a normal number for 0..253; anything for NaN blocks
+    return __uint_as_float((254u - scale_byte) << 23);
 }
 __device__ __forceinline__ float mx_scale(uint32_t scale_byte) {
     return scale_byte == 255u ? __uint_as_float(0x7FC00000u) : scale_byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(scale_byte << 23);
@@ -87,14 +87,25 @@ __device__ __forceinline__ uint32_t mx_codes4_e4m3(float a, float b, float c, fl
            (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
 }
 __device__ __forceinline__ uint32_t mx_codes2_e2m1(float a, float b) { return __nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest); }
-// 8 numbers -> 8 bytes (e4m3) or 4 bytes in .x (e2m1); a NaN block's numbers are all 0 here
+// two products at once
+__device__ __forceinline__ float2 times(float a, float b, float f) {
+    uint64_t v, g;
+    float2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(g) : "f"(f));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(v), "l"(g));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+// 8 numbers -> 8 bytes (e4m3) or 4 bytes in .x (e2m1)
 template <int FMT>
 __device__ __forceinline__ uint2 mx_codes8(const float (&v)[8], float inverse) {
-    float t[8];
+    float2 t[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = inverse == 0.f ? 0.f : __fmul_rn(v[i], inverse);
-    if (FMT == MX_E4M3) return make_uint2(mx_codes4_e4m3(t[0], t[1], t[2], t[3]), mx_codes4_e4m3(t[4], t[5], t[6], t[7]));
-    return make_uint2(mx_codes2_e2m1(t[0], t[1]) | mx_codes2_e2m1(t[2], t[3]) << 8 | mx_codes2_e2m1(t[4], t[5]) << 16 | mx_codes2_e2m1(t[6], t[7]) << 24, 0u);
+    for (int i = 0; i < 4; ++i) t[i] = times(v[2 * i], v[2 * i + 1], inverse);
+    if (FMT == MX_E4M3) return make_uint2(mx_codes4_e4m3(t[0].x, t[0].y, t[1].x, t[1].y), mx_codes4_e4m3(t[2].x, t[2].y, t[3].x, t[3].y));
+    return make_uint2(mx_codes2_e2m1(t[0].x, t[0].y) | mx_codes2_e2m1(t[1].x, t[1].y) << 8 | mx_codes2_e2m1(t[2].x, t[2].y) << 16 |
+                          mx_codes2_e2m1(t[3].x, t[3].y) << 24, 0u);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -108,6 +119,20 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
+// the larger magnitude of each half of two words, a NaN above all
+template <typename T> __device__ __forceinline__ uint32_t larger_of_each(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t larger_of_each<__nv_bfloat16>(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2_nan(__habs2(*reinterpret_cast<const __nv_bfloat162*>(&a)), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <> __device__ __forceinline__ uint32_t larger_of_each<__half>(uint32_t a, uint32_t b) {
+    const __half2 m = __hmax2_nan(__habs2(*reinterpret_cast<const __half2*>(&a)), __habs2(*reinterpret_cast<const __half2*>(&b)));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <typename T> __device__ __forceinline__ float half_of(uint32_t w, uint32_t which) {
+    const unsigned short h = (unsigned short)(w >> (16u * which));
+    return to_f32(*reinterpret_cast<const T*>(&h));
+}
 template <typename T> struct Row8;          // raw: 8 numbers as they are in memory
 template <> struct Row8<float> {
     uint4 a, b;
@@ -119,6 +144,13 @@ template <> struct Row8<float> {
     __device__ __forceinline__ void set(const float (&v)[8]) {
         a = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
         b = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    }
+    __device__ __forceinline__ uint32_t largest() const {          // magnitude, as a float's bits
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+        return m;
     }
     __device__ __forceinline__ void load(const float* p) {
         a = *reinterpret_cast<const uint4*>(p);
@@ -145,6 +177,10 @@ template <typename T> struct Row8 {          // the 16-bit types
         for (int i = 0; i < 4; ++i) w[i] = word(from_f32<T>(v[2 * i])) | word(from_f32<T>(v[2 * i + 1])) << 16;
         a = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ __forceinline__ uint32_t largest() const {
+        const uint32_t m = larger_of_each<T>(larger_of_each<T>(a.x, a.y), larger_of_each<T>(a.z, a.w));
+        return max(magnitude(half_of<T>(m, 0u)), magnitude(half_of<T>(m, 1u)));
+    }
     __device__ __forceinline__ void load(const T* p) { a = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = a; }
 
@@ -166,6 +202,164 @@ __device__ __forceinline__ void store8_any(T* p, uint32_t left, const float (&v)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if ((uint32_t)i < left) p[i] = from_f32<T>(v[i]);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rows that do not begin at multiples of 16 bytes, by whole 16-byte units all the same: a unit of the row is cut from two aligned ones.
+// (Number by number a warp's store touches 16 sectors for 64 bytes: the norm of 2000 x 4097 bf16 took 41 us that way, its backward 71.)
+// ---------------------------------------------------------------------------------------------
+template <typename T> struct Units {
+    static constexpr uint32_t E = 16u / sizeof(T);                 // numbers of a unit
+    static __device__ __forceinline__ uint32_t offset(const T* p) { return (uint32_t)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); }
+    // E numbers of a and b, one behind the other, from number s (< E) on
+    static __device__ __forceinline__ uint4 cut(const uint4& a, const uint4& b, uint32_t s) {
+        const uint32_t words = sizeof(T) == 4 ? s : s >> 1;
+        uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        if (words & 2u) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) x[i] = x[i + 2];
+        }
+        if (words & 1u) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) x[i] = x[i + 1];
+        }
+        if (sizeof(T) == 2 && (s & 1u)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __funnelshift_r(x[i], x[i + 1], 16);
+        }
+        return make_uint4(x[0], x[1], x[2], x[3]);
+    }
+    static __device__ __forceinline__ T number(const uint4& q, uint32_t i) {        // (i known when compiled)
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        if (sizeof(T) == 4) return *reinterpret_cast<const T*>(&w[i & 3u]);
+        const unsigned short h = (unsigned short)(w[(i >> 1) & 3u] >> (16u * (i & 1u)));
+        return *reinterpret_cast<const T*>(&h);
+    }
+    // numbers [lo, hi) of a unit, one by one
+    static __device__ __forceinline__ void put(T* p, const uint4& q, uint32_t lo, uint32_t hi) {
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i)
+            if (i >= lo && i < hi) p[i] = number(q, i);
+    }
+    // N units from p on, of which `left` numbers are there (the rest: 0), in two steps, so that many reads can be under way together:
+    // ask() reads the aligned units that they lie in, take() cuts them out.  The matrix lies between `begin` and `end`: nothing outside is
+    // read (a row's neighbours may be); what lies at its own two ends is read by take(), number by number.
+    template <int N> static __device__ __forceinline__ bool inside(const T* p, const T* begin, const T* end) {
+        const uint32_t o = offset(p);
+        return p - o >= begin && p - o + (o ? N + 1 : N) * E <= end;
+    }
+    template <int N> static __device__ __forceinline__ void ask(const T* p, const T* begin, const T* end, uint32_t left, uint4 (&a)[N + 1]) {
+        const uint32_t o = offset(p);
+        const uint4* at = reinterpret_cast<const uint4*>(p - o);
+        const bool in = left != 0u && inside<N>(p, begin, end);
+#pragma unroll
+        for (int u = 0; u <= N; ++u) {
+            a[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (in && (u < N || o != 0u)) a[u] = at[u];
+        }
+    }
+    template <int N> static __device__ __forceinline__ void take(const T* p, const T* begin, const T* end, uint32_t left, const uint4 (&a)[N + 1], uint4 (&q)[N]) {
+        const uint32_t o = offset(p);
+#pragma unroll
+        for (int u = 0; u < N; ++u) q[u] = cut(a[u], a[u + 1], o);
+        if (left != 0u && (left < N * E || !inside<N>(p, begin, end))) {
+            const bool in = inside<N>(p, begin, end);
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (uint32_t i = 0; i < E; ++i) {
+                    if (u * E + i < left) {
+                        const T v = in ? number(q[u], i) : p[u * E + i];
+                        if (sizeof(T) == 4) w[i & 3u] = *reinterpret_cast<const uint32_t*>(&v);
+                        else w[(i >> 1) & 3u] |= (uint32_t)*reinterpret_cast<const unsigned short*>(&v) << (16u * (i & 1u));
+                    }
+                }
+                q[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+    // N units to p on, of which `left` numbers are wanted (0: none).  All lanes of the warp together; a lane's successor holds what
+    // follows in the same row, unless it is the `last` of its run (`first`: no lane before it does so).
+    template <int N>
+    static __device__ __forceinline__ void store(T* p, uint32_t left, const uint4 (&own)[N], bool first, bool last) {
+        uint4 next;
+        next.x = __shfl_down_sync(0xFFFFFFFFu, own[0].x, 1);
+        next.y = __shfl_down_sync(0xFFFFFFFFu, own[0].y, 1);
+        next.z = __shfl_down_sync(0xFFFFFFFFu, own[0].z, 1);
+        next.w = __shfl_down_sync(0xFFFFFFFFu, own[0].w, 1);
+        uint32_t left_next = __shfl_down_sync(0xFFFFFFFFu, left, 1);
+        if (last) left_next = 0u;
+        const uint32_t o = offset(p), s = o ? E - o : 0u;             // numbers before the first aligned unit
+        const bool joins = left >= N * E && left_next >= s;           // the last unit, with the next lane's first s numbers
+        bool joined = __shfl_up_sync(0xFFFFFFFFu, joins ? 1 : 0, 1) != 0;
+        if (first) joined = false;
+        if (left == 0u) return;
+        if (!joined) put(p, own[0], 0u, min(s, left));
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const bool whole = u < N - 1 ? left >= (u + 1u) * E + s : joins;
+            if (whole) {
+                *reinterpret_cast<uint4*>(p + s + u * E) = cut(own[u], u < N - 1 ? own[u + 1 < N ? u + 1 : u] : next, s);
+            } else if (left > u * E) {
+                put(p + u * E, own[u], s, left - u * E);
+                if (u < N - 1 && left > (u + 1u) * E) put(p + (u + 1u) * E, own[u + 1 < N ? u + 1 : u], 0u, min(s, left - (u + 1u) * E));
+            }
+        }
+    }
+};
+// Row8 <-> units
+template <typename T> struct Raw8 { static constexpr int N = sizeof(T) == 4 ? 2 : 1; };
+__device__ __forceinline__ void to_units(const Row8<float>& r, uint4 (&q)[2]) { q[0] = r.a, q[1] = r.b; }
+template <typename T> __device__ __forceinline__ void to_units(const Row8<T>& r, uint4 (&q)[1]) { q[0] = r.a; }
+__device__ __forceinline__ void from_units(const uint4 (&q)[2], Row8<float>& r) { r.a = q[0], r.b = q[1]; }
+template <typename T> __device__ __forceinline__ void from_units(const uint4 (&q)[1], Row8<T>& r) { r.a = q[0]; }
+// a matrix to read from: where it begins and ends, numbers between two rows
+template <typename T> struct Rows {
+    const T *begin, *end;
+    uint64_t stride;
+    __device__ __forceinline__ Rows(const void* x, uint32_t rows, uint32_t cols, uint64_t s)
+        : begin(static_cast<const T*>(x)), end(static_cast<const T*>(x) + (rows - 1u) * s + cols), stride(s) {}
+};
+// 8 numbers of a row on their way; VEC: they begin at a multiple of 16 bytes and are all there (or none is)
+template <typename T, bool VEC> struct Asked8 {
+    static constexpr int N = Raw8<T>::N;
+    uint4 a[VEC ? N : N + 1];
+    __device__ __forceinline__ void ask(const Rows<T>& m, uint64_t row, uint32_t at, uint32_t left) {
+        const T* p = m.begin + (left ? row * m.stride + at * 8u : 0u);
+        if constexpr (VEC) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                a[u] = make_uint4(0u, 0u, 0u, 0u);
+                if (left) a[u] = reinterpret_cast<const uint4*>(p)[u];
+            }
+        } else {
+            Units<T>::template ask<N>(p, m.begin, m.end, left, a);
+        }
+    }
+    __device__ __forceinline__ void take(const Rows<T>& m, uint64_t row, uint32_t at, uint32_t left, Row8<T>& r) const {
+        if constexpr (VEC) {
+            from_units(a, r);
+        } else {
+            uint4 q[N];
+            Units<T>::template take<N>(m.begin + (left ? row * m.stride + at * 8u : 0u), m.begin, m.end, left, a, q);
+            from_units(q, r);
+        }
+    }
+    __device__ __forceinline__ void take(const Rows<T>& m, uint64_t row, uint32_t at, uint32_t left, float (&v)[8]) const {
+        Row8<T> r;
+        take(m, row, at, left, r);
+        r.get(v);
+    }
+};
+// all lanes of the warp together, each with the 8 numbers behind its predecessor's
+template <typename T>
+__device__ __forceinline__ void store8_row(T* p, uint32_t left, const float (&v)[8]) {
+    Row8<T> r;
+    r.set(v);
+    uint4 q[Raw8<T>::N];
+    to_units(r, q);
+    Units<T>::store(p, left, q, (threadIdx.x & 31u) == 0u, (threadIdx.x & 31u) == 31u);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -38,7 +38,7 @@ struct MxProductParams {
     uint32_t swapped;            // the lanes are columns of out
     uint32_t out_dtype;
     uint32_t split;              // CTAs of a cluster
-    uint32_t vec;                // out: 16-byte stores along a row
+    uint32_t vec;                // out: rows begin at multiples of 16 bytes
 };
 struct MxCtl {
     uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES], done, taken;      // done: a tile is summed; taken: it is in registers
@@ -178,6 +178,36 @@ __device__ __forceinline__ void mxp_out_any(const MxProductParams& p, uint32_t r
     if (p.out_dtype == DIV_BF16) mxp_out<__nv_bfloat16>(p, row_p, row_s, n, v);
     else if (p.out_dtype == DIV_F16) mxp_out<__half>(p, row_p, row_s, n, v);
     else mxp_out<float>(p, row_p, row_s, n, v);
+}
+
+// C numbers of a row of out, of which `left` are there, in 16-byte stores wherever the row begins
+template <typename OT, uint32_t C>
+__device__ __forceinline__ void mxp_row(OT* to, uint32_t left, const uint32_t (&raw)[(C + 31u) / 32u][32], bool good) {
+    typedef Units<OT> U;
+    const uint32_t o = U::offset(to), s = o ? U::E - o : 0u;
+    const auto unit = [&](uint32_t u) {
+        OT v[U::E];
+#pragma unroll
+        for (uint32_t i = 0; i < U::E; ++i) {
+            const uint32_t c = u * U::E + i;
+            v[i] = from_f32<OT>(good ? __uint_as_float(raw[c / 32u][c % 32u]) : __uint_as_float(0x7FC00000u));
+        }
+        return *reinterpret_cast<const uint4*>(v);
+    };
+    uint4 one = unit(0);
+    U::put(to, one, 0u, min(s, left));
+#pragma unroll
+    for (uint32_t u = 0; u < C / U::E; ++u) {
+        const bool more = u + 1u < C / U::E;
+        const uint4 next = more ? unit(u + 1u) : make_uint4(0u, 0u, 0u, 0u);
+        if (left >= (u + 1u) * U::E + s && (more || s == 0u)) {
+            *reinterpret_cast<uint4*>(to + u * U::E + s) = U::cut(one, next, s);
+        } else if (left > u * U::E) {
+            U::put(to + u * U::E, one, s, left - u * U::E);
+            if (more && left > (u + 1u) * U::E) U::put(to + (u + 1u) * U::E, next, 0u, min(s, left - (u + 1u) * U::E));
+        }
+        one = next;
+    }
 }
 
 template <int FMT, uint32_t BN>
@@ -321,6 +351,17 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl->taken);
+            if (p.split == 1u && !p.swapped) {
+                const uint32_t i = p0 + row, j = s0 + c0;
+                if (i < p.p.s.rows && j < p.s.s.rows) {
+                    const uint64_t at = (uint64_t)i * p.ld + j;
+                    const uint32_t left = p.s.s.rows - j;
+                    if (p.out_dtype == DIV_BF16) mxp_row<__nv_bfloat16, T::MINE>(static_cast<__nv_bfloat16*>(p.out) + at, left, raw, good);
+                    else if (p.out_dtype == DIV_F16) mxp_row<__half, T::MINE>(static_cast<__half*>(p.out) + at, left, raw, good);
+                    else mxp_row<float, T::MINE>(static_cast<float*>(p.out) + at, left, raw, good);
+                }
+                continue;
+            }
 #pragma unroll
             for (uint32_t c = 0; c < T::MINE; c += 32u) {
                 float v[32];

@@ -15,7 +15,13 @@ namespace divk {
 
 constexpr int NORM_NONE = -1;                   // no blob
 constexpr uint32_t NORM_MAX_THREADS = 512, NORM_MAX_HELD = 16384;       // a thread holds at most 4 pieces of 8 in a row of 512 threads
-constexpr uint32_t NORM_BWD_CTAS = 148 * 2;
+// Backward's CTAs stay for many rows: as many as fit an SM, by the threads of each (what a thread holds takes 64 registers with one
+// piece, 128 with two, 102 where that lets two CTAs of 320 threads in).  More CTAs than fit, or fewer, took longer: 16384 x 4096
+// bf16 with 256 threads 161, 97, 119, 101 us for 1, 2, 3, 4 CTAs an SM.
+constexpr uint32_t NORM_SMS = 148;
+__host__ __device__ constexpr uint32_t norm_resident(int held, uint32_t threads) {
+    return held == 1 ? 1024u / threads : held == 2 ? (threads <= 256u ? 512u / threads : threads <= 320u ? 2u : 1u) : 1u;
+}
 
 struct NormParams {
     const void *x, *residual, *w;
@@ -44,66 +50,68 @@ __device__ __forceinline__ float norm_sum(float v, uint32_t group, float* shared
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     return v;
 }
+// 8 numbers of a row from `at` * 8 on; `left` of them are there
 template <typename T, bool VEC>
-__device__ __forceinline__ void norm_load(const T* p, uint32_t left, float (&v)[8]) {
-    if (VEC) {
-        Row8<T> r;
-        r.load(p);
-        r.get(v);
-    } else {
-        load8_any(p, left, v);
-    }
+__device__ __forceinline__ void norm_load(const Rows<T>& m, uint64_t row, uint32_t at, uint32_t left, float (&v)[8]) {
+    Asked8<T, VEC> a;
+    a.ask(m, row, at, left);
+    a.take(m, row, at, left, v);
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void norm_raw(const T* p, uint32_t left, Row8<T>& r) {
-    if (VEC) {
-        r.load(p);
-    } else {
-        float v[8];
-        load8_any(p, left, v);
-        r.set(v);                       // (exact: they come from T)
-    }
-}
+// all lanes of a warp together, with pieces that follow one another; left 0: nothing
 template <typename T, bool VEC>
 __device__ __forceinline__ void norm_store(T* p, uint32_t left, const float (&v)[8]) {
     if (VEC) {
-        Row8<T> r;
-        r.set(v);
-        r.store(p);
+        if (left) {
+            Row8<T> r;
+            r.set(v);
+            r.store(p);
+        }
     } else {
-        store8_any(p, left, v);
+        store8_row(p, left, v);
     }
 }
-// h of piece `at` of a row: added in 32 bits, rounded, and stored where there is a residual
-template <typename XT, bool VEC>
-__device__ __forceinline__ void norm_h(const NormParams& p, uint32_t row, uint32_t at, float (&h)[8]) {
-    const uint32_t left = p.cols - at * 8u;
-    norm_load<XT, VEC>(static_cast<const XT*>(p.x) + row * p.x_stride + at * 8u, left, h);
-    if (p.residual) {
-        float r[8];
-        norm_load<XT, VEC>(static_cast<const XT*>(p.residual) + row * p.r_stride + at * 8u, left, r);
+__device__ __forceinline__ uint32_t norm_left(bool there, uint32_t at, uint32_t cols) { return there && at * 8u < cols ? cols - at * 8u : 0u; }
+
+// h of `M` pieces of a row, `group` apart from `at` on: added in 32 bits, rounded, and stored where there is a residual (as norm_store)
+template <typename XT, bool VEC, int M>
+__device__ __forceinline__ void norm_h(const NormParams& p, uint32_t row, bool there, uint32_t at, float (&h)[M][8]) {
+    const Rows<XT> x(p.x, p.rows, p.cols, p.x_stride), r(p.residual, p.rows, p.cols, p.r_stride);
+    Asked8<XT, VEC> ax[M], ar[M];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = to_f32(from_f32<XT>(h[i] + r[i]));
-        norm_store<XT, VEC>(static_cast<XT*>(p.h) + (uint64_t)row * p.cols + at * 8u, left, h);
+    for (int j = 0; j < M; ++j) {
+        const uint32_t left = norm_left(there, at + j * p.group, p.cols);
+        ax[j].ask(x, row, at + j * p.group, left);
+        if (p.residual) ar[j].ask(r, row, at + j * p.group, left);
+    }
+#pragma unroll
+    for (int j = 0; j < M; ++j) {
+        const uint32_t here = at + j * p.group, left = norm_left(there, here, p.cols);
+        ax[j].take(x, row, here, left, h[j]);
+        if (p.residual) {
+            float v[8];
+            ar[j].take(r, row, here, left, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[j][i] = to_f32(from_f32<XT>(h[j][i] + v[i]));
+            norm_store<XT, VEC>(static_cast<XT*>(p.h) + (uint64_t)row * p.cols + here * 8u, left, h[j]);
+        }
     }
 }
-// y of a piece, and its codes.  All lanes of a warp come here with pieces that follow one another.
+// y of a piece, and its codes (as norm_store)
 template <typename XT, typename WT, int FMT, bool VEC>
 __device__ __forceinline__ void norm_out(const NormParams& p, uint32_t row, bool row_there, uint32_t at, const float (&h)[8], float rstd) {
-    const bool there = row_there && at * 8u < p.cols;
+    const uint32_t left = norm_left(row_there, at, p.cols);
     float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (there) {
-        const uint32_t left = p.cols - at * 8u;
+    if (left) {
         float w[8];
-        norm_load<WT, VEC>(static_cast<const WT*>(p.w) + at * 8u, left, w);
+        norm_load<WT, VEC>(Rows<WT>(p.w, 1u, p.cols, 0u), 0u, at, left, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = h[i] * rstd * w[i];
         if (!VEC) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = (uint32_t)i < left ? y[i] : 0.f;      // (0 times an infinite rstd would be NaN)
         }
-        if (p.y) norm_store<XT, VEC>(static_cast<XT*>(p.y) + (uint64_t)row * p.cols + at * 8u, left, y);
     }
+    if (p.y) norm_store<XT, VEC>(static_cast<XT*>(p.y) + (uint64_t)row * p.cols + at * 8u, left, y);
     if (FMT != NORM_NONE) {
         constexpr int F = FMT == NORM_NONE ? 0 : FMT;
         uint32_t big = 0;
@@ -142,13 +150,7 @@ norm_forward_kernel(const __grid_constant__ NormParams p) {
     if (HELD) {
         float h[HELD ? HELD : 1][8];
         float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < HELD; ++j) {
-            const uint32_t at = j * p.group + t;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[j][i] = 0.f;
-            if (there && at * 8u < p.cols) norm_h<XT, VEC>(p, row, at, h[j]);
-        }
+        norm_h<XT, VEC>(p, row, there, t, h);
 #pragma unroll
         for (int j = 0; j < HELD; ++j)
 #pragma unroll
@@ -162,10 +164,10 @@ norm_forward_kernel(const __grid_constant__ NormParams p) {
         const uint32_t rounds = (p.pieces + p.group - 1u) / p.group;
         for (uint32_t j = 0; j < rounds; ++j) {
             const uint32_t at = j * p.group + t;
-            float h[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (there && at * 8u < p.cols) norm_h<XT, VEC>(p, row, at, h);
+            float h[1][8];
+            norm_h<XT, VEC>(p, row, there, at, h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(h[i], h[i], sum);
+            for (int i = 0; i < 8; ++i) sum = fmaf(h[0][i], h[0][i], sum);
         }
         const float rstd = 1.0f / sqrtf(norm_sum(sum, p.group, shared) / (float)p.cols + p.eps);
         if (there && t == 0 && p.rstd) p.rstd[row] = rstd;
@@ -173,9 +175,9 @@ norm_forward_kernel(const __grid_constant__ NormParams p) {
             const uint32_t at = j * p.group + t;
             float h[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (there && at * 8u < p.cols) {
-                // (this thread's own writes)
-                if (p.residual) norm_load<XT, VEC>(static_cast<const XT*>(p.h) + (uint64_t)row * p.cols + at * 8u, p.cols - at * 8u, h);
-                else norm_load<XT, VEC>(static_cast<const XT*>(p.x) + row * p.x_stride + at * 8u, p.cols - at * 8u, h);
+                // (written by this CTA, before the barriers of the sum)
+                if (p.residual) norm_load<XT, VEC>(Rows<XT>(static_cast<const XT*>(p.h) + (uint64_t)row * p.cols, 1u, p.cols, 0u), 0u, at, p.cols - at * 8u, h);
+                else norm_load<XT, VEC>(Rows<XT>(p.x, p.rows, p.cols, p.x_stride), row, at, p.cols - at * 8u, h);
             }
             norm_out<XT, WT, FMT, VEC>(p, row, there, at, h, rstd);
         }
@@ -192,8 +194,8 @@ struct NormBackParams {
     uint32_t group;
 };
 
-template <typename XT, typename WT, bool VEC, int HELD>
-__global__ void __launch_bounds__(NORM_MAX_THREADS)
+template <typename XT, typename WT, bool VEC, int HELD, uint32_t THREADS>       // THREADS: at most
+__global__ void __launch_bounds__(THREADS, norm_resident(HELD, THREADS))
 norm_backward_kernel(const __grid_constant__ NormBackParams p) {
     __shared__ float shared[32];
     const uint32_t per = blockDim.x / p.group, t = threadIdx.x % p.group, mine = blockIdx.x * per + threadIdx.x / p.group;
@@ -210,21 +212,17 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[j][i] = 0.f;
         // the next row's dy and h are under way while this one is summed and written
-        Row8<XT> dy[N], h[N], dh[N];
+        Asked8<XT, VEC> dy[N], h[N], dh[N];
         float rstd = 0.f, next_rstd = 0.f;
+        const Rows<XT> all_dy(p.dy, p.rows, p.cols, p.dy_stride), all_h(p.h, p.rows, p.cols, p.h_stride), all_dh(p.dh, p.rows, p.cols, p.dh_stride);
         const auto bring = [&](uint32_t k) {
             const uint64_t row = (uint64_t)k * step + mine;
-            const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             next_rstd = row < p.rows ? p.rstd[row] : 0.f;
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
-                const uint32_t at = j * p.group + t;
-                dy[j].set(zero);
-                h[j].set(zero);
-                if (row < p.rows && at * 8u < p.cols) {
-                    norm_raw<XT, VEC>(static_cast<const XT*>(p.dy) + row * p.dy_stride + at * 8u, p.cols - at * 8u, dy[j]);
-                    norm_raw<XT, VEC>(static_cast<const XT*>(p.h) + row * p.h_stride + at * 8u, p.cols - at * 8u, h[j]);
-                }
+                const uint32_t at = j * p.group + t, left = norm_left(row < p.rows, at, p.cols);
+                dy[j].ask(all_dy, row, at, left);
+                h[j].ask(all_h, row, at, left);
             }
         };
         bring(0);
@@ -234,15 +232,17 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
             float g[N][8], n[N][8];
             float dot = 0.f;
             rstd = next_rstd;
+            if (p.dh) {
+#pragma unroll
+                for (int j = 0; j < HELD; ++j) dh[j].ask(all_dh, row, j * p.group + t, norm_left(there, j * p.group + t, p.cols));
+            }
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
-                const uint32_t at = j * p.group + t;
-                if (p.dh && there && at * 8u < p.cols)
-                    norm_raw<XT, VEC>(static_cast<const XT*>(p.dh) + row * p.dh_stride + at * 8u, p.cols - at * 8u, dh[j]);
+                const uint32_t at = j * p.group + t, left = norm_left(there, at, p.cols);
                 float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (at * 8u < p.cols) norm_load<WT, VEC>(static_cast<const WT*>(p.w) + at * 8u, p.cols - at * 8u, w);
-                dy[j].get(g[j]);
-                h[j].get(n[j]);
+                if (at * 8u < p.cols) norm_load<WT, VEC>(Rows<WT>(p.w, 1u, p.cols, 0u), 0u, at, p.cols - at * 8u, w);
+                dy[j].take(all_dy, row, at, left, g[j]);
+                h[j].take(all_h, row, at, left, n[j]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     n[j][i] *= rstd;
@@ -255,21 +255,19 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
             const float mean = norm_sum(dot, p.group, shared) * inv;
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
-                const uint32_t at = j * p.group + t;
-                if (there && at * 8u < p.cols) {
-                    float d[8], add[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    if (p.dh) dh[j].get(add);
+                const uint32_t at = j * p.group + t, left = norm_left(there, at, p.cols);
+                float d[8], add[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (p.dh) dh[j].take(all_dh, row, at, left, add);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, fmaf(-n[j][i], mean, g[j][i]), add[i]);
-                    norm_store<XT, VEC>(static_cast<XT*>(p.dx) + row * p.cols + at * 8u, p.cols - at * 8u, d);
-                }
+                for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, fmaf(-n[j][i], mean, g[j][i]), add[i]);
+                norm_store<XT, VEC>(static_cast<XT*>(p.dx) + row * p.cols + at * 8u, left, d);
             }
         }
         if (p.sums) {
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
                 const uint32_t at = j * p.group + t;
-                if (at * 8u < p.cols) norm_store<float, VEC>(sums + at * 8u, p.cols - at * 8u, acc[j]);
+                norm_store<float, VEC>(sums + at * 8u, norm_left(true, at, p.cols), acc[j]);
             }
         }
     } else {
@@ -281,18 +279,18 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
             const float rstd = there ? p.rstd[row] : 0.f;
             float dot = 0.f, mean = 0.f;
             for (int pass = 0; pass < 2; ++pass) {
-                for (uint32_t at = t; at < pieces && there; at += p.group) {
-                    const uint32_t left = p.cols - at * 8u;
-                    float g[8], n[8], w[8], add[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    norm_load<XT, VEC>(static_cast<const XT*>(p.dy) + row * p.dy_stride + at * 8u, left, g);
-                    norm_load<XT, VEC>(static_cast<const XT*>(p.h) + row * p.h_stride + at * 8u, left, n);
-                    norm_load<WT, VEC>(static_cast<const WT*>(p.w) + at * 8u, left, w);
-                    if (pass && p.dh) norm_load<XT, VEC>(static_cast<const XT*>(p.dh) + row * p.dh_stride + at * 8u, left, add);
-                    float sum[8], d[8];
-                    if (pass && p.sums && k) norm_load<float, VEC>(sums + at * 8u, left, sum);
-                    else
+                for (uint32_t j = 0; j * p.group < pieces; ++j) {
+                    const uint32_t at = j * p.group + t, left = norm_left(there, at, p.cols);
+                    float g[8], n[8], w[8], add[8], sum[8], d[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+                    for (int i = 0; i < 8; ++i) g[i] = n[i] = w[i] = add[i] = sum[i] = 0.f;
+                    if (left) {
+                        norm_load<XT, VEC>(Rows<XT>(p.dy, p.rows, p.cols, p.dy_stride), row, at, left, g);
+                        norm_load<XT, VEC>(Rows<XT>(p.h, p.rows, p.cols, p.h_stride), row, at, left, n);
+                        norm_load<WT, VEC>(Rows<WT>(p.w, 1u, p.cols, 0u), 0u, at, left, w);
+                        if (pass && p.dh) norm_load<XT, VEC>(Rows<XT>(p.dh, p.rows, p.cols, p.dh_stride), row, at, left, add);
+                        if (pass && p.sums && k) load8_any(sums + at * 8u, left, sum);          // (this thread's own writes)
+                    }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         n[i] *= rstd;
@@ -303,7 +301,7 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
                     }
                     if (pass) {
                         norm_store<XT, VEC>(static_cast<XT*>(p.dx) + row * p.cols + at * 8u, left, d);
-                        if (p.sums) norm_store<float, VEC>(sums + at * 8u, left, sum);
+                        if (p.sums && left) store8_any(sums + at * 8u, left, sum);
                     }
                 }
                 if (!pass) mean = norm_sum(dot, p.group, shared) * inv;
@@ -385,9 +383,10 @@ struct NormBack {
 NormBack norm_back(int64_t rows, int64_t cols) {
     NormBack b;
     b.s = norm_split(((uint64_t)cols + 7u) / 8u, (uint64_t)rows);
-    const uint32_t per = b.s.threads / b.s.group;
+    uint32_t per = b.s.threads / b.s.group;
     const uint64_t all = ((uint64_t)rows + per - 1u) / per;
-    const uint64_t most = b.s.threads >= 512u ? NORM_BWD_CTAS : NORM_BWD_CTAS * 2u;
+    if (b.s.held == 4u) b.s = {NORM_MAX_THREADS, 0u, NORM_MAX_THREADS};             // (too many registers with gradients)
+    const uint64_t most = b.s.held ? NORM_SMS * norm_resident((int)b.s.held, b.s.threads) : NORM_SMS * 2u;
     b.grid = (uint32_t)(all < most ? all : most);
     b.parts = b.grid * per;
     return b;
@@ -479,10 +478,12 @@ div_status div_rms_norm_backward(const void* dy_dev, int64_t dy_row_stride, cons
         typedef std::remove_pointer_t<decltype(x)> XT;
         typedef std::remove_pointer_t<decltype(w)> WT;
         cudaStream_t st = (cudaStream_t)cuda_stream;
-        auto kern = b.s.held == 0   ? (vec ? norm_backward_kernel<XT, WT, true, 0> : norm_backward_kernel<XT, WT, false, 0>)
-                    : b.s.held == 1 ? (vec ? norm_backward_kernel<XT, WT, true, 1> : norm_backward_kernel<XT, WT, false, 1>)
-                    : b.s.held == 2 ? (vec ? norm_backward_kernel<XT, WT, true, 2> : norm_backward_kernel<XT, WT, false, 2>)
-                                    : (vec ? norm_backward_kernel<XT, WT, true, 4> : norm_backward_kernel<XT, WT, false, 4>);
+        void (*kern)(const NormBackParams);
+        if (b.s.held == 0) kern = vec ? norm_backward_kernel<XT, WT, true, 0, 512> : norm_backward_kernel<XT, WT, false, 0, 512>;
+        else if (b.s.held == 1) kern = vec ? norm_backward_kernel<XT, WT, true, 1, 512> : norm_backward_kernel<XT, WT, false, 1, 512>;
+        else if (b.s.threads <= 256) kern = vec ? norm_backward_kernel<XT, WT, true, 2, 256> : norm_backward_kernel<XT, WT, false, 2, 256>;
+        else if (b.s.threads <= 320) kern = vec ? norm_backward_kernel<XT, WT, true, 2, 320> : norm_backward_kernel<XT, WT, false, 2, 320>;
+        else kern = vec ? norm_backward_kernel<XT, WT, true, 2, 512> : norm_backward_kernel<XT, WT, false, 2, 512>;
         const div_status got = launch_pdl(kern, dim3(b.grid), b.s.threads, 0, st, p);
         if (got != DIV_OK || !dweight_dev) return got;
         return launch_pdl(norm_weight_kernel<WT>, dim3((uint32_t)(((uint64_t)cols + 31u) / 32u)), 1024, 0, st, (const float*)workspace_dev, b.parts,
