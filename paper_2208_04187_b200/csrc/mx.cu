@@ -6,9 +6,12 @@
 // Both are bound by memory: x is read once, 1 + 1/32 or 1/2 + 1/32 bytes a number are written for each direction.
 //
 // A CTA takes 128 x 128 numbers, which are whole tiles of e4m3 codes in both directions (half tiles of e2m1).  A thread reads
-// 8 neighbours at a time, 8 times, all reads under way together; 4 lanes hold a block, whose largest magnitude takes two
-// shuffles.  For the columns the numbers go through shared memory as they are; a thread then owns 32 rows of one column
-// (two columns of 16-bit types, one word), and its codes go through shared memory once more, so that whole lines leave the SM.
+// 8 neighbours at a time, 8 times, all reads under way together, and leaves them in shared memory as they are.  From there a
+// thread takes whole blocks: 32 neighbours of a row, 32 rows of a column (of two columns of 16-bit types, one word).  So a
+// scale costs its dozen instructions once a block; what bounds the kernel next to memory is the issue of instructions (with 8 numbers of
+// a block to a thread and shuffles, 75 % of the issue slots at 8192 x 4096).  The columns' codes go through shared memory once more, so
+// that whole lines leave the SM.  In a row of shared memory the 16-byte pieces of a block are permuted, so that neither way meets
+// bank conflicts: piece j of block b of row r is at j ^ mxq_turn(r, b).
 #include "mx.cuh"
 
 namespace divk {
@@ -24,8 +27,12 @@ struct MxQuantParams {
 };
 
 template <typename XT> __host__ __device__ constexpr uint32_t mxq_smem_bytes(bool cols) {
-    // numbers; codes by columns as their tile lies in the blob; scales by columns
-    return 512u + (cols ? MXQ_TILE * MXQ_TILE * (uint32_t)sizeof(XT) + 16384u + 512u : 0u);
+    // scales by rows; numbers; codes by columns as their tile lies in the blob; scales by columns
+    return 512u + MXQ_TILE * MXQ_TILE * (uint32_t)sizeof(XT) + (cols ? 16384u + 512u : 0u);
+}
+// 4 pieces of 8 numbers or 8 of 4: the 8 lanes that a shared-memory access serves together hold 4 blocks of two rows
+template <typename XT> __device__ __forceinline__ uint32_t mxq_turn(uint32_t row, uint32_t block) {
+    return sizeof(XT) == 4 ? block ^ (row & 1u) << 2 : block >> 1 ^ (row & 1u) << 1;
 }
 
 template <typename XT, int FMT, bool ROWS, bool COLS, bool VEC>
@@ -33,7 +40,7 @@ __global__ void __launch_bounds__(MXQ_THREADS)
 mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
     typedef MxFormat<FMT> F;
     extern __shared__ __align__(128) unsigned char smem[];
-    uint32_t* row_scales = reinterpret_cast<uint32_t*>(smem);
+    unsigned char* row_scales = smem;
     XT* numbers = reinterpret_cast<XT*>(smem + 512);
     unsigned char* codes = smem + 512 + MXQ_TILE * MXQ_TILE * sizeof(XT);
     unsigned char* col_scales = codes + 16384;
@@ -63,40 +70,69 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
             a[i].take(x, r, c / 8u, r < p.r.rows ? left : 0u, raw[i0 + i]);
         }
     }
-    if (COLS) {
+    constexpr uint32_t PIECES = sizeof(XT) == 4 ? 8u : 4u, PITCH = MXQ_TILE * (uint32_t)sizeof(XT);       // 16-byte pieces of a block; bytes of a row
+    unsigned char* tile_of = reinterpret_cast<unsigned char*>(numbers);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) raw[i].store(numbers + (row_in + 16u * i) * MXQ_TILE + lane16 * 8u);
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t r = row_in + 16u * i, block = lane16 >> 2, turn = mxq_turn<XT>(r, block), first = (lane16 & 3u) * (PIECES / 4u);
+        uint4 q[Raw8<XT>::N];
+        to_units(raw[i], q);
+#pragma unroll
+        for (uint32_t u = 0; u < PIECES / 4u; ++u)
+            *reinterpret_cast<uint4*>(tile_of + r * PITCH + (block * PIECES + ((first + u) ^ turn)) * 16u) = q[u];
     }
+    __syncthreads();
     if (ROWS) {
         const uint32_t stage = c0 / F::STAGE, atom = (c0 % F::STAGE) / 128u;
         unsigned char* tile = p.by_rows + mx_tile_offset(p.r, ty, stage);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t rt = row_in + 16u * i;
-            float v[8];
-            raw[i].get(v);
-            uint32_t big = raw[i].largest();
-            big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
-            big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
-            const uint32_t e = mx_scale_byte<FMT>(big);
-            const uint2 q = mx_codes8<FMT>(v, mx_inverse(e));
-            if (r0 + rt < p.r.rows) {
-                if (FMT == MX_E4M3) *reinterpret_cast<uint2*>(tile + mx_piece(rt, lane16 >> 1) + (lane16 & 1u) * 8u) = q;
-                else *reinterpret_cast<uint32_t*>(tile + mx_piece(rt, atom * 4u + (lane16 >> 2)) + (lane16 & 3u) * 4u) = q.x;
+        for (uint32_t t = threadIdx.x; t < 512u; t += MXQ_THREADS) {
+            const uint32_t r = t >> 2, block = t & 3u, turn = mxq_turn<XT>(r, block);
+            uint32_t e = 0u;
+            if (r0 + r < p.r.rows) {
+                uint4 q[PIECES];
+#pragma unroll
+                for (uint32_t j = 0; j < PIECES; ++j) q[j] = *reinterpret_cast<const uint4*>(tile_of + r * PITCH + (block * PIECES + (j ^ turn)) * 16u);
+                uint32_t big = 0u;
+                if constexpr (sizeof(XT) == 2) {
+                    uint32_t m = larger_of_each<XT>(larger_of_each<XT>(q[0].x, q[0].y), larger_of_each<XT>(q[0].z, q[0].w));
+#pragma unroll
+                    for (uint32_t j = 1; j < PIECES; ++j)
+                        m = larger_of_each<XT>(m, larger_of_each<XT>(larger_of_each<XT>(q[j].x, q[j].y), larger_of_each<XT>(q[j].z, q[j].w)));
+                    big = max(magnitude(half_of<XT>(m, 0u)), magnitude(half_of<XT>(m, 1u)));
+                } else {
+#pragma unroll
+                    for (uint32_t j = 0; j < PIECES; ++j)
+                        big = max(big, max(max(q[j].x & 0x7FFFFFFFu, q[j].y & 0x7FFFFFFFu), max(q[j].z & 0x7FFFFFFFu, q[j].w & 0x7FFFFFFFu)));
+                }
+                e = mx_scale_byte<FMT>(big);
+                const float inverse = mx_inverse(e);
+                uint2 codes8[4];
+#pragma unroll
+                for (uint32_t h = 0; h < 4; ++h) {
+                    uint4 some[Raw8<XT>::N];
+#pragma unroll
+                    for (uint32_t u = 0; u < PIECES / 4u; ++u) some[u] = q[h * (PIECES / 4u) + u];
+                    Row8<XT> eight;
+                    from_units(some, eight);
+                    float v[8];
+                    eight.get(v);
+                    codes8[h] = mx_codes8<FMT>(v, inverse);
+                }
+                if (FMT == MX_E4M3) {
+                    *reinterpret_cast<uint4*>(tile + mx_piece(r, 2u * block)) = make_uint4(codes8[0].x, codes8[0].y, codes8[1].x, codes8[1].y);
+                    *reinterpret_cast<uint4*>(tile + mx_piece(r, 2u * block + 1u)) = make_uint4(codes8[2].x, codes8[2].y, codes8[3].x, codes8[3].y);
+                } else {
+                    *reinterpret_cast<uint4*>(tile + mx_piece(r, atom * 4u + block)) = make_uint4(codes8[0].x, codes8[1].x, codes8[2].x, codes8[3].x);
+                }
             }
-            // the 4 scales of a row in one word
-            uint32_t word = e << ((lane16 >> 2) * 8u);
-            word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
-            word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
-            if (lane16 == 0) row_scales[mx_scale_slot(rt) >> 2] = word;
+            row_scales[mx_scale_slot(r) + block] = (unsigned char)e;
         }
         __syncthreads();
         if (threadIdx.x < 128u) {
             uint32_t* to = reinterpret_cast<uint32_t*>(p.by_rows + mx_scales_at(p.r) + (((uint64_t)ty * p.r.stages + stage) * F::ATOMS + atom) * 512u);
-            if (r0 < p.r.rows) to[threadIdx.x] = row_scales[threadIdx.x];
+            if (r0 < p.r.rows) to[threadIdx.x] = reinterpret_cast<const uint32_t*>(row_scales)[threadIdx.x];
         }
-    } else {
-        __syncthreads();
     }
     if (COLS) {
         if (c0 >= p.r.cols) return;                                // (the tile is there for the blob by rows alone)
@@ -106,9 +142,13 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
         for (uint32_t t = threadIdx.x; t < TASKS; t += MXQ_THREADS) {
             const uint32_t col = t % (128u / W) * W, block = t / (128u / W);
             uint32_t word[32];
-            const XT* from = numbers + block * 32u * MXQ_TILE + col;
+            // (even rows turn their pieces one way, odd ones the other)
+            constexpr uint32_t E = 16u / (uint32_t)sizeof(XT);
+            const uint32_t across = col >> 5, j = (col & 31u) / E, in = (col % E) * (uint32_t)sizeof(XT);
+            const unsigned char* even = tile_of + block * 32u * PITCH + (across * PIECES + (j ^ mxq_turn<XT>(0u, across))) * 16u + in;
+            const unsigned char* odd = tile_of + block * 32u * PITCH + (across * PIECES + (j ^ mxq_turn<XT>(1u, across))) * 16u + in;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) word[i] = *reinterpret_cast<const uint32_t*>(from + i * MXQ_TILE);
+            for (int i = 0; i < 32; ++i) word[i] = *reinterpret_cast<const uint32_t*>(((i & 1) ? odd : even) + i * PITCH);
             uint32_t big_of_each = word[0];                        // of the column, or of the two
             if constexpr (W == 2) {
 #pragma unroll
@@ -144,9 +184,9 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
         }
         __syncthreads();
         unsigned char* tile = p.by_cols + mx_tile_offset(p.c, tx, stage);
-        constexpr uint32_t PIECES = FMT == MX_E4M3 ? 8u : 4u;
-        for (uint32_t t = threadIdx.x; t < 128u * PIECES; t += MXQ_THREADS) {
-            const uint32_t row = t / PIECES, at = mx_piece(row, (FMT == MX_E4M3 ? 0u : atom * 4u) + t % PIECES);
+        constexpr uint32_t OUT = FMT == MX_E4M3 ? 8u : 4u;             // pieces of codes in a row
+        for (uint32_t t = threadIdx.x; t < 128u * OUT; t += MXQ_THREADS) {
+            const uint32_t row = t / OUT, at = mx_piece(row, (FMT == MX_E4M3 ? 0u : atom * 4u) + t % OUT);
             if (c0 + row < p.c.rows) *reinterpret_cast<uint4*>(tile + at) = *reinterpret_cast<const uint4*>(codes + at);
         }
         if (threadIdx.x < 128u) {
@@ -225,8 +265,8 @@ div_status quantize_launch(const MxQuantParams& p, bool rows, bool cols, bool ve
         rows ? (cols ? (vec ? mx_quantize_kernel<XT, FMT, true, true, true> : mx_quantize_kernel<XT, FMT, true, true, false>)
                      : (vec ? mx_quantize_kernel<XT, FMT, true, false, true> : mx_quantize_kernel<XT, FMT, true, false, false>))
              : (vec ? mx_quantize_kernel<XT, FMT, false, true, true> : mx_quantize_kernel<XT, FMT, false, true, false>);
-    static SmemAllowed allowed[4];
-    if (cols && !allowed[(rows ? 2 : 0) + (vec ? 1 : 0)]((const void*)kern, smem)) return DIV_ERR_CUDA;
+    static SmemAllowed allowed[8];
+    if (smem > 48u * 1024u && !allowed[(cols ? 4 : 0) + (rows ? 2 : 0) + (vec ? 1 : 0)]((const void*)kern, smem)) return DIV_ERR_CUDA;
     return launch_pdl(kern, dim3(grid), MXQ_THREADS, smem, st, p);
 }
 

@@ -15,7 +15,9 @@ backward pass is the quantised form of its input, 8.25 or 4.25 bits a number, an
 
 Glue only, as in `autograd`: every step, of backward passes too, runs in the CUDA library through the C ABI (include/division.h says what it
 computes), on the current stream of the inputs' device.  Inputs are CUDA tensors of dtype float32, bfloat16 or float16; leading
-dimensions are folded into rows.  Rows that are runs of neighbours are read where they are, whatever their stride.
+dimensions are folded into rows.  Rows that are runs of neighbours are read where they are, whatever their stride.  The calls may
+be captured into CUDA graphs; a backward pass only while no eager graph of the same leaves is alive, as with any operator of
+torch (its accumulation nodes tie the eager stream to the capture, which torch refuses).
 """
 from __future__ import annotations
 

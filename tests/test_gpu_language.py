@@ -180,3 +180,55 @@ def test_two_streams_at_once():
                 got.append(chain(x))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for p, q in zip(got, want) for a, b in zip(p, q))
+
+
+def test_a_gradient_has_no_gradient():
+    x, w = make(8, 64, seed=1).cuda().requires_grad_(), make(16, 64, seed=2).cuda().requires_grad_()
+    t = torch.arange(8, device="cuda")
+    for y in (lm.mx_linear(x, w), lm.rms_norm(x, w[0])[0], lm.token_logprobs(x, t).logprobs, lm.mx_norm_linear(x, w[0], w)[0]):
+        (g,) = torch.autograd.grad(y.float().sum(), x, create_graph=True)
+        assert g.isfinite().all()
+        with pytest.raises(RuntimeError, match="has no gradient"):
+            g.float().sum().backward()
+
+
+def test_a_training_step_is_captured_and_replayed():
+    """Forward and backward in one graph (no eager graph of the same leaves is alive: torch would tie the legacy stream to the capture)."""
+    d, vocab = 128, 300
+    g, w = torch.ones(d, device="cuda", dtype=torch.bfloat16).requires_grad_(), make(vocab, d, seed=1).cuda().requires_grad_()
+    x, t = make(40, d, seed=2).cuda().requires_grad_(), torch.arange(40, device="cuda")
+    dl = torch.full((40,), -1 / 40, device="cuda")
+
+    def step():
+        out, _ = lm.mx_norm_linear(x, g, w)
+        got = lm.token_logprobs(out, t)
+        return (got.logprobs, *torch.autograd.grad(got.logprobs, (x, g, w), dl))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    with torch.no_grad():
+        x.copy_(make(40, d, seed=3).cuda())
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, step()))
+
+
+def test_saved_tensors_are_watched():
+    x, g = make(8, 64, seed=1).cuda().requires_grad_(), torch.ones(64, device="cuda", dtype=torch.bfloat16)
+    z = x * 1
+    y, _ = lm.rms_norm(z, g)
+    z.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.float().sum().backward()
+    z = x * 1
+    w = make(16, 64, seed=2).cuda()
+    y = lm.mx_linear(z, w.requires_grad_())
+    with torch.no_grad():
+        z.zero_()                                       # (its quantised form alone is kept)
+    dw = torch.autograd.grad(y.float().sum(), w)[0]
+    assert dw.abs().sum() > 0
