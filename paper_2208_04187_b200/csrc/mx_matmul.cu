@@ -17,33 +17,11 @@
 //
 // Every wait is bounded (MXP_LIMIT_NS): a CTA that gives up waits for its copies, gives its tensor memory back, and
 // writes NaN for its tile.
-#include "mx.cuh"
+#include "mx_product.cuh"
 
 namespace divk {
 
-constexpr uint32_t MXP_OUT_WARPS = 8, MXP_PRODUCER = 8, MXP_ISSUER = 9, MXP_THREADS = 320;
-constexpr uint32_t MXP_MAX_STAGES = 8, MXP_SMS = 148;
-constexpr uint64_t MXP_LIMIT_NS = 2000000000ull;
-constexpr uint32_t MXP_SMEM = 224u * 1024u;       // of a CTA, ring and control block
-
-struct MxSide {
-    const unsigned char *codes, *scales;
-    MxShape s;
-};
-struct MxProductParams {
-    MxSide p, s;
-    void* out;
-    uint64_t ld;                 // numbers between two rows of out
-    uint32_t tiles_p, tiles;
-    uint32_t swapped;            // the lanes are columns of out
-    uint32_t out_dtype;
-    uint32_t split;              // CTAs of a cluster
-    uint32_t vec;                // out: rows begin at multiples of 16 bytes
-};
-struct MxCtl {
-    uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES], done, taken;      // done: a tile is summed; taken: it is in registers
-    uint32_t tmem, failed;
-};
+constexpr uint32_t MXP_THREADS = 320;
 
 template <int FMT, uint32_t BN> struct MxTile {
     typedef MxFormat<FMT> F;
@@ -63,10 +41,6 @@ template <int FMT, uint32_t BN> struct MxTile {
     static_assert(BN == 256u || STAGES * STAGE_BYTES >= 128u * BN * 4u, "a split tile waits in the ring");
 };
 
-// shared-memory matrix descriptor: start, stride between groups of 8 rows; version 1 of the layout
-__device__ __forceinline__ uint64_t mxp_desc(uint32_t at, uint32_t group_bytes, uint64_t swizzle) {
-    return (uint64_t)((at & 0x3FFFFu) >> 4) | (uint64_t)1u << 16 | (uint64_t)(group_bytes >> 4) << 32 | 1ull << 46 | swizzle << 61;
-}
 template <int FMT>
 __device__ __forceinline__ void mxp_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
     if (FMT == MX_E2M1)
@@ -88,128 +62,6 @@ __device__ __forceinline__ void mxp_scales(uint32_t columns, uint64_t desc) {   
 __device__ __forceinline__ void mxp_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void mxp_load32(uint32_t at, uint32_t (&v)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
-        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
-        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-        : "r"(at)
-        : "memory");
-}
-__device__ __forceinline__ void mxp_load16(uint32_t at, uint32_t (&v)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(at)
-        : "memory");
-}
-// waits for a phase, at most MXP_LIMIT_NS, and not once another thread of the CTA has given up
-__device__ __forceinline__ bool mxp_wait(uint64_t* bar, uint32_t parity, MxCtl* ctl) {
-    uint64_t t0 = 0;
-    for (uint32_t polls = 1;; ++polls) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((polls & 63u) == 0u) {                         // (reading the timer takes longer than most waits)
-            const uint64_t t = now_ns();
-            if (t0 == 0u) t0 = t;
-            if (*(volatile uint32_t*)&ctl->failed || t - t0 > MXP_LIMIT_NS) {
-                *(volatile uint32_t*)&ctl->failed = 1u;
-                return false;
-            }
-        }
-    }
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// an address in the shared memory of another CTA of the cluster; a number there (whose writing a cluster barrier has ordered before)
-__device__ __forceinline__ uint32_t cluster_at(uint32_t local, uint32_t rank) {
-    uint32_t at;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
-    return at;
-}
-__device__ __forceinline__ float ld_cluster(uint32_t at) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
-    return v;
-}
-
-template <typename OT>
-__device__ __forceinline__ void mxp_store_run(OT* to, const float (&v)[32], uint32_t count, bool vec) {
-#pragma unroll
-    for (uint32_t g = 0; g < 32u; g += 8u) {
-        float w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = v[g + k];
-        if (vec && g + 8u <= count) {
-            Row8<OT> r;
-            r.set(w);
-            r.store(to + g);
-        } else if (g < count) {
-            store8_any(to + g, count - g, w);
-        }
-    }
-}
-template <typename OT>
-__device__ __forceinline__ void mxp_out(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
-    if (row_p >= p.p.s.rows || row_s >= p.s.s.rows) return;
-    const uint32_t count = min(n, p.s.s.rows - row_s);
-    OT* out = static_cast<OT*>(p.out);
-    if (p.swapped) {
-        OT* to = out + (uint64_t)row_s * p.ld + row_p;
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if ((uint32_t)i < count) to[i * p.ld] = from_f32<OT>(v[i]);
-    } else {
-        mxp_store_run(out + (uint64_t)row_p * p.ld + row_s, v, count, p.vec && (row_s & 7u) == 0u);
-    }
-}
-__device__ __forceinline__ void mxp_out_any(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
-    if (p.out_dtype == DIV_BF16) mxp_out<__nv_bfloat16>(p, row_p, row_s, n, v);
-    else if (p.out_dtype == DIV_F16) mxp_out<__half>(p, row_p, row_s, n, v);
-    else mxp_out<float>(p, row_p, row_s, n, v);
-}
-
-// C numbers of a row of out, of which `left` are there, in 16-byte stores wherever the row begins
-template <typename OT, uint32_t C>
-__device__ __forceinline__ void mxp_row(OT* to, uint32_t left, const uint32_t (&raw)[(C + 31u) / 32u][32], bool good) {
-    typedef Units<OT> U;
-    const uint32_t o = U::offset(to), s = o ? U::E - o : 0u;
-    const auto unit = [&](uint32_t u) {
-        OT v[U::E];
-#pragma unroll
-        for (uint32_t i = 0; i < U::E; ++i) {
-            const uint32_t c = u * U::E + i;
-            v[i] = from_f32<OT>(good ? __uint_as_float(raw[c / 32u][c % 32u]) : __uint_as_float(0x7FC00000u));
-        }
-        return *reinterpret_cast<const uint4*>(v);
-    };
-    uint4 one = unit(0);
-    U::put(to, one, 0u, min(s, left));
-#pragma unroll
-    for (uint32_t u = 0; u < C / U::E; ++u) {
-        const bool more = u + 1u < C / U::E;
-        const uint4 next = more ? unit(u + 1u) : make_uint4(0u, 0u, 0u, 0u);
-        if (left >= (u + 1u) * U::E + s && (more || s == 0u)) {
-            *reinterpret_cast<uint4*>(to + u * U::E + s) = U::cut(one, next, s);
-        } else if (left > u * U::E) {
-            U::put(to + u * U::E, one, s, left - u * U::E);
-            if (more && left > (u + 1u) * U::E) U::put(to + (u + 1u) * U::E, next, 0u, min(s, left - (u + 1u) * U::E));
-        }
-        one = next;
-    }
-}
-
 template <int FMT, uint32_t BN>
 __global__ void __launch_bounds__(MXP_THREADS, 1)
 mx_product_kernel(const __grid_constant__ MxProductParams p) {
@@ -615,15 +467,25 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     if (format == MX_E2M1 && p.s.s.rows == 1u && (uint64_t)p.p.s.rows * p.p.s.stages <= MXV_MOST && p.p.s.stages <= MXV_MAX_SMEM / mxv_smem(1u)) return vector_launch(p, (cudaStream_t)cuda_stream);
     p.vec = aligned_16(out_dev) && (m == 1 || out_row_stride * size % 16 == 0);
     const uint64_t rows_s = p.s.s.rows;
-    p.tiles_p = (p.p.s.rows + 127u) / 128u;
+    const uint64_t blocks_p = (p.p.s.rows + 127u) / 128u;
     uint32_t bn = rows_s <= 16 ? 16u : rows_s <= 32 ? 32u : rows_s <= 64 ? 64u : 128u;
-    if (bn == 128u && (uint64_t)p.tiles_p * ((rows_s + 255u) / 256u) >= 120u) bn = 256u;
-    const uint64_t tiles = p.tiles_p * ((rows_s + bn - 1u) / bn);
+    if (bn == 128u && blocks_p * ((rows_s + 255u) / 256u) >= 120u) bn = 256u;
+    const uint64_t across = (rows_s + bn - 1u) / bn, tiles = blocks_p * across;
+    if (tiles >= (1ull << 31)) return DIV_ERR_SHAPE;
+    p.tiles_p = (uint32_t)blocks_p;
+    p.tiles = (uint32_t)tiles;
+    p.split = 1;
+    // large products of e2m1: by pairs of CTAs, whose start and end take longer than they save with rows of less than 4096 numbers or fewer
+    // than two rounds of tiles (mx_pair.cu has both sides' times; it counts rows of 128 bytes in 31 bits)
+    const uint64_t paired = (blocks_p + 1u) / 2u * across;
+    if (format == MX_E2M1 && bn == 256u && p.p.s.stages >= 16u && paired >= MXP_SMS && ((mx_codes_bytes(p.p.s) | mx_codes_bytes(p.s.s)) >> 38) == 0) {
+        p.tiles_p = (uint32_t)((blocks_p + 1u) / 2u);
+        p.tiles = (uint32_t)paired;
+        return mx_pair_launch(p, (cudaStream_t)cuda_stream);
+    }
     uint32_t split = 1;
     while (bn < 256u && split < 8u && tiles * split * 2u <= 160u && p.p.s.stages >= 4u * split) split *= 2u;
     p.split = split;
-    if (tiles >= (1ull << 31)) return DIV_ERR_SHAPE;
-    p.tiles = (uint32_t)tiles;
     const uint32_t grid = split > 1u ? (uint32_t)tiles * split : (uint32_t)(tiles < MXP_SMS ? tiles : MXP_SMS);
     return format == MX_E4M3 ? product_by_width<MX_E4M3>(bn, p, grid, (cudaStream_t)cuda_stream)
                              : product_by_width<MX_E2M1>(bn, p, grid, (cudaStream_t)cuda_stream);

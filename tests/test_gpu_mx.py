@@ -188,3 +188,19 @@ def test_a_long_matrix_passes_32_bits():
     p = lm.mx_matmul(q, one, torch.float32)
     assert float(p[rows - 1, 0]) == lo.mx_values(np.arange(64.0)[None], "e2m1").sum() and float(p[rows - 300, 0]) == 96.0
     assert int(torch.count_nonzero(p)) == 2
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m, n, k", [(3000, 3100, 4096), (2944, 3585, 4100), (4100, 2305, 8000), (2561, 4000, 3850)])
+def test_large_products_of_4_bits(m, n, k, dtype):
+    """Tiles by pairs of CTAs: odd numbers of blocks, cut blocks, rows of out that begin anywhere.  Sums of these products are exact in 32 bits
+    (numbers of one size: every product is a multiple of the smallest, and sums stay below 2^24 of it), so nothing but the rounding is left."""
+    g = torch.Generator("cuda").manual_seed(m)
+    a = torch.randint(-6, 7, (m, k), generator=g, device="cuda").float()
+    b = torch.randint(-6, 7, (n, k), generator=g, device="cuda").float()
+    a[:, ::32], b[:, ::32] = 6, 6                                   # every block's scale is 1
+    qa, qb = lm.mx_quantize(a, "e2m1"), lm.mx_quantize(b, "e2m1")
+    want = qa.dequantize(torch.float32).double() @ qb.dequantize(torch.float32).double().t()
+    y = lm.mx_matmul(qa, qb, TYPES[dtype])
+    assert torch.equal(y, want.to(TYPES[dtype]))
+    assert torch.equal(lm.mx_matmul(qa, qb, TYPES[dtype]), y)
