@@ -468,9 +468,9 @@ const char* div_status_string(div_status s) {
     switch (s) {
         case DIV_OK: return "ok";
         case DIV_ERR_NULL: return "null pointer";
-        case DIV_ERR_SHAPE: return "bad shape (need n,c,h,w >= 1, c*h*w < 2^32, n < 2^31)";
-        case DIV_ERR_PARAM: return "bad parameter (block >= 1, qbits in {1,2,4,8}, dtype in {f32,bf16})";
-        case DIV_ERR_ALIGN: return "device pointer not 16-byte aligned";
+        case DIV_ERR_SHAPE: return "bad shape (maps: n,c,h,w >= 1, c*h*w < 2^32, n < 2^31; matrices: rows, cols in 1 .. 2^31 - 513, no row stride below a row)";
+        case DIV_ERR_PARAM: return "bad parameter (maps: block >= 1, qbits in {1,2,4,8}, dtype in {f32,bf16}; matrices: dtype in {f32,bf16,f16}, format in {e4m3,e2m1})";
+        case DIV_ERR_ALIGN: return "device pointer not aligned (16 bytes; numbers of matrices: their size)";
         case DIV_ERR_CAPACITY: return "buffer too small";
         case DIV_ERR_CUDA: return "CUDA runtime error";
         case DIV_ERR_TIMEOUT: return "device-side bounded wait expired";
