@@ -28,7 +28,8 @@ struct MxQuantParams {
 
 template <typename XT> __host__ __device__ constexpr uint32_t mxq_smem_bytes(bool cols) {
     // scales by rows; numbers; codes by columns as their tile lies in the blob; scales by columns
-    return 512u + MXQ_TILE * MXQ_TILE * (uint32_t)sizeof(XT) + (cols ? 16384u + 512u : 0u);
+    // (16-bit types: in the place of the numbers, which all threads have in registers by then; so 6 CTAs fit an SM instead of 4)
+    return 512u + MXQ_TILE * MXQ_TILE * (uint32_t)sizeof(XT) + (cols ? (sizeof(XT) == 4 ? 16384u : 0u) + 512u : 0u);
 }
 // 4 pieces of 8 numbers or 8 of 4: the 8 lanes that a shared-memory access serves together hold 4 blocks of two rows
 template <typename XT> __device__ __forceinline__ uint32_t mxq_turn(uint32_t row, uint32_t block) {
@@ -42,8 +43,8 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* row_scales = smem;
     XT* numbers = reinterpret_cast<XT*>(smem + 512);
-    unsigned char* codes = smem + 512 + MXQ_TILE * MXQ_TILE * sizeof(XT);
-    unsigned char* col_scales = codes + 16384;
+    unsigned char* codes = smem + 512 + (sizeof(XT) == 4 ? MXQ_TILE * MXQ_TILE * sizeof(XT) : 0u);
+    unsigned char* col_scales = smem + 512 + MXQ_TILE * MXQ_TILE * sizeof(XT) + (sizeof(XT) == 4 ? 16384u : 0u);
 
     const uint32_t tx = blockIdx.x % p.tiles_x, ty = blockIdx.x / p.tiles_x;
     const uint32_t r0 = ty * MXQ_TILE, c0 = tx * MXQ_TILE;
@@ -149,6 +150,10 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
             const unsigned char* odd = tile_of + block * 32u * PITCH + (across * PIECES + (j ^ mxq_turn<XT>(1u, across))) * 16u + in;
 #pragma unroll
             for (int i = 0; i < 32; ++i) word[i] = *reinterpret_cast<const uint32_t*>(((i & 1) ? odd : even) + i * PITCH);
+            if constexpr (W == 2) {                                // (as many tasks as threads)
+                static_assert(TASKS == MXQ_THREADS, "one task a thread");
+                __syncthreads();
+            }
             uint32_t big_of_each = word[0];                        // of the column, or of the two
             if constexpr (W == 2) {
 #pragma unroll

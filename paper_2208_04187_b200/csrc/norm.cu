@@ -114,25 +114,23 @@ __device__ __forceinline__ void norm_out(const NormParams& p, uint32_t row, bool
     if (p.y) norm_store<XT, VEC>(static_cast<XT*>(p.y) + (uint64_t)row * p.cols + at * 8u, left, y);
     if (FMT != NORM_NONE) {
         constexpr int F = FMT == NORM_NONE ? 0 : FMT;
-        uint32_t big = 0;
+        float most = fabsf(y[0]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) big = max(big, magnitude(y[i]));
+        for (int i = 1; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(y[i])));
+        uint32_t big = __float_as_uint(most);                                          // (a NaN's bits order above all)
         big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
         big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
         const uint32_t e = mx_scale_byte<F>(big);
         const uint2 q = mx_codes8<F>(y, mx_inverse(e));
-        uint32_t word = e << ((at >> 2 & 3u) * 8u);                                   // scales of 128 numbers, 16 pieces
-        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
-        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
         if (row_there && at < p.pieces) {
             constexpr uint32_t PER = MxFormat<F>::STAGE / 8u;
             const uint32_t rb = row >> 7, rt = row & 127u, stage = at / PER, in = at % PER;
             unsigned char* tile = p.blob + mx_tile_offset(p.s, rb, stage);
             if (F == MX_E4M3) *reinterpret_cast<uint2*>(tile + mx_piece(rt, in >> 1) + (in & 1u) * 8u) = q;
             else *reinterpret_cast<uint32_t*>(tile + mx_piece(rt, in >> 2) + (in & 3u) * 4u) = q.x;
-            if ((at & 15u) == 0)
-                *reinterpret_cast<uint32_t*>(p.blob + mx_scales_at(p.s) + (((uint64_t)rb * p.s.stages + stage) * MxFormat<F>::ATOMS + in / 16u) * 512u +
-                                             mx_scale_slot(rt)) = word;
+            if ((at & 3u) == 0u)
+                p.blob[mx_scales_at(p.s) + (((uint64_t)rb * p.s.stages + stage) * MxFormat<F>::ATOMS + in / 16u) * 512u + mx_scale_slot(rt) + (in / 4u & 3u)] =
+                    (unsigned char)e;
         }
     }
 }
