@@ -56,7 +56,7 @@ mx_quantize_kernel(const __grid_constant__ MxQuantParams p) {
 
     Row8<XT> raw[8];
     const Rows<XT> x(p.x, p.r.rows, p.r.cols, p.stride);
-    constexpr int AT_ONCE = VEC || sizeof(XT) == 2 ? 8 : 4;                    // (what lies unaligned takes more registers on its way)
+    constexpr int AT_ONCE = VEC ? 8 : 4;                                       // (what lies unaligned takes more registers on its way)
 #pragma unroll
     for (int i0 = 0; i0 < 8; i0 += AT_ONCE) {
         Asked8<XT, VEC> a[AT_ONCE];

@@ -33,10 +33,10 @@ namespace divk {
 constexpr int MX_E4M3 = 0, MX_E2M1 = 1;
 template <int FMT> struct MxFormat;
 template <> struct MxFormat<MX_E4M3> {
-    static constexpr uint32_t STAGE = 128, ATOMS = 1, BLOCK_BYTES = 32;   // numbers of a row in a stage; atoms of scales for it
+    static constexpr uint32_t STAGE = 128, ATOMS = 1;   // numbers of a row in a stage; atoms of scales for it
 };
 template <> struct MxFormat<MX_E2M1> {
-    static constexpr uint32_t STAGE = 256, ATOMS = 2, BLOCK_BYTES = 16;
+    static constexpr uint32_t STAGE = 256, ATOMS = 2;
 };
 __host__ __device__ inline uint32_t mx_stage(int fmt) { return fmt == MX_E4M3 ? 128u : 256u; }
 
@@ -145,13 +145,6 @@ template <> struct Row8<float> {
         a = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
         b = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
     }
-    __device__ __forceinline__ uint32_t largest() const {          // magnitude, as a float's bits
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
-        return m;
-    }
     __device__ __forceinline__ void load(const float* p) {
         a = *reinterpret_cast<const uint4*>(p);
         b = *(reinterpret_cast<const uint4*>(p) + 1);
@@ -176,10 +169,6 @@ template <typename T> struct Row8 {          // the 16-bit types
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = word(from_f32<T>(v[2 * i])) | word(from_f32<T>(v[2 * i + 1])) << 16;
         a = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    __device__ __forceinline__ uint32_t largest() const {
-        const uint32_t m = larger_of_each<T>(larger_of_each<T>(a.x, a.y), larger_of_each<T>(a.z, a.w));
-        return max(magnitude(half_of<T>(m, 0u)), magnitude(half_of<T>(m, 1u)));
     }
     __device__ __forceinline__ void load(const T* p) { a = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = a; }
@@ -279,6 +268,32 @@ template <typename T> struct Units {
             }
         }
     }
+    // the first n (< E) numbers of a unit to p, a multiple of 16 bytes; the last n to where p ends, another: in stores of 8, 4 and 2 bytes
+    static __device__ __forceinline__ void put_first(T* p, const uint4& q, uint32_t n) {
+        uint32_t words = n, at = 0;
+        if (sizeof(T) == 2) words = n >> 1;
+        uint32_t* w = reinterpret_cast<uint32_t*>(p);
+        if (words & 2u) {
+            *reinterpret_cast<uint2*>(w) = make_uint2(q.x, q.y);
+            at = 2;
+        }
+        if (words & 1u) w[at] = at ? q.z : q.x;
+        if (sizeof(T) == 2 && (n & 1u)) {
+            const uint32_t last = words == 0u ? q.x : words == 1u ? q.y : words == 2u ? q.z : q.w;
+            reinterpret_cast<unsigned short*>(p)[n - 1u] = (unsigned short)last;
+        }
+    }
+    static __device__ __forceinline__ void put_last(T* end, const uint4& q, uint32_t n) {        // numbers 0 .. n-1 of q
+        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+        T* p = end - n;
+        if (sizeof(T) == 2 && (n & 1u)) *reinterpret_cast<unsigned short*>(p) = (unsigned short)q.x;
+        const uint32_t odd = sizeof(T) == 2 ? n & 1u : 0u, one = sizeof(T) == 2 ? 2u : 1u;         // numbers of a word
+        if (n & one) *reinterpret_cast<uint32_t*>(p + odd) = cut(q, none, odd).x;
+        if (n & (2u * one)) {
+            const uint4 r = cut(q, none, n & (2u * one - 1u));
+            *reinterpret_cast<uint2*>(p + (n & (2u * one - 1u))) = make_uint2(r.x, r.y);
+        }
+    }
     // N units to p on, of which `left` numbers are wanted (0: none).  All lanes of the warp together; a lane's successor holds what
     // follows in the same row, unless it is the `last` of its run (`first`: no lane before it does so).
     template <int N>
@@ -295,12 +310,17 @@ template <typename T> struct Units {
         bool joined = __shfl_up_sync(0xFFFFFFFFu, joins ? 1 : 0, 1) != 0;
         if (first) joined = false;
         if (left == 0u) return;
-        if (!joined) put(p, own[0], 0u, min(s, left));
+        if (!joined) {
+            if (left >= s) put_last(p + s, own[0], s);
+            else put(p, own[0], 0u, left);
+        }
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const bool whole = u < N - 1 ? left >= (u + 1u) * E + s : joins;
             if (whole) {
                 *reinterpret_cast<uint4*>(p + s + u * E) = cut(own[u], u < N - 1 ? own[u + 1 < N ? u + 1 : u] : next, s);
+            } else if (u == N - 1 && left >= N * E) {
+                put_first(p + s + u * E, cut(own[u], make_uint4(0u, 0u, 0u, 0u), s), E - s);
             } else if (left > u * E) {
                 put(p + u * E, own[u], s, left - u * E);
                 if (u < N - 1 && left > (u + 1u) * E) put(p + (u + 1u) * E, own[u + 1 < N ? u + 1 : u], 0u, min(s, left - (u + 1u) * E));

@@ -104,7 +104,8 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
         for (uint32_t tile = first; tile < p.tiles && ok; tile += step) {
             const uint32_t tp = tile % p.tiles_p, s0 = tile / p.tiles_p * BN;
             const uint32_t hp = mx_tile_rows(p.p.s, tp) * 128u;
-            // rows of S: of its only block of 128 (BN < 128), or BN / 128 whole blocks
+            // rows of S: of its only block of 128 (BN < 128), or whole blocks.  (A narrow tile inside a larger block would want its scales at
+            // another column of tensor memory than a multiple of 4, which the instruction answered with a misaligned address.)
             uint32_t hs[T::S_BLOCKS], step_s[T::S_BLOCKS];
             const unsigned char *from_s[T::S_BLOCKS], *scales_s[T::S_BLOCKS];
             uint32_t bytes = hp + T::SCALES;
@@ -176,7 +177,8 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) {
                     const uint32_t atom = FMT == MX_E2M1 ? i >> 1 : 0u, id = FMT == MX_E2M1 ? (i & 1u) * 2u : i;
-                    mxp_mma<FMT>(tmem, dp + 2u * i, ds + 2u * i, idesc0 | id << 4 | id << 29, cp + 4u * atom, cs + 4u * T::S_BLOCKS * atom, k != k0 || i != 0u);
+                    mxp_mma<FMT>(tmem, dp + 2u * i, ds + 2u * i, idesc0 | id << 4 | id << 29, cp + 4u * atom, cs + 4u * T::S_BLOCKS * atom,
+                                 k != k0 || i != 0u);
                 }
                 mxp_commit(&ctl->empty[slot]);
             }
@@ -204,14 +206,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl->taken);
             if (p.split == 1u && !p.swapped) {
-                const uint32_t i = p0 + row, j = s0 + c0;
-                if (i < p.p.s.rows && j < p.s.s.rows) {
-                    const uint64_t at = (uint64_t)i * p.ld + j;
-                    const uint32_t left = p.s.s.rows - j;
-                    if (p.out_dtype == DIV_BF16) mxp_row<__nv_bfloat16, T::MINE>(static_cast<__nv_bfloat16*>(p.out) + at, left, raw, good);
-                    else if (p.out_dtype == DIV_F16) mxp_row<__half, T::MINE>(static_cast<__half*>(p.out) + at, left, raw, good);
-                    else mxp_row<float, T::MINE>(static_cast<float*>(p.out) + at, left, raw, good);
-                }
+                mxp_row_any<T::MINE>(p, p0 + row, s0 + c0, T::MINE, raw, good);
                 continue;
             }
 #pragma unroll
@@ -220,7 +215,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = (T::MINE >= 32u || i < 16) ? (good ? __uint_as_float(raw[c / 32u][i]) : __uint_as_float(0x7FC00000u)) : 0.f;
                 if (p.split == 1u) {
-                    mxp_out_any(p, p0 + row, s0 + c0 + c, min(T::MINE, 32u), v);
+                    mxp_column_any(p, p0 + row, s0 + c0 + c, min(T::MINE, 32u), v);
                 } else {
                     float* part = reinterpret_cast<float*>(ring);       // [column][lane]; all copies and products are through
 #pragma unroll
@@ -237,11 +232,14 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             // this CTA's share of the columns, half of it for each four warps; reads of 8 columns of two CTAs are under way together
             const uint32_t mine = BN / p.split / 2u, c0 = rank * 2u * mine + (warp >> 2) * mine, row = (warp & 3u) * 32u + lane;
             const uint32_t p0 = first % p.tiles_p * 128u, s0 = first / p.tiles_p * BN;
-            for (uint32_t c = 0; c < mine; c += 8u) {
-                const uint32_t n = min(mine - c, 8u), at = smem_u32(ring) + ((c0 + c) * 128u + row) * 4u;
-                float v[32], one[8], two[8];
+            float v[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            for (uint32_t c = 0; c < 32u; c += 8u) {
+                const uint32_t n = c < mine ? min(mine - c, 8u) : 0u, at = smem_u32(ring) + ((c0 + c) * 128u + row) * 4u;
+                float one[8], two[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c + i] = 0.f;
+                if (n == 0u) continue;
                 for (uint32_t r = 0; r < p.split; r += 2u) {
                     const uint32_t at1 = cluster_at(at, r), at2 = cluster_at(at, r + 1u);
 #pragma unroll
@@ -250,9 +248,16 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
                         two[i] = i < n ? ld_cluster(at2 + i * 512u) : 0.f;
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = (v[i] + one[i]) + two[i];
+                    for (int i = 0; i < 8; ++i) v[c + i] = (v[c + i] + one[i]) + two[i];
                 }
-                mxp_out_any(p, p0 + row, s0 + c0 + c, n, v);
+            }
+            if (p.swapped) {
+                mxp_column_any(p, p0 + row, s0 + c0, mine, v);
+            } else {
+                uint32_t raw[1][32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) raw[0][i] = __float_as_uint(v[i]);
+                mxp_row_any<32>(p, p0 + row, s0 + c0, mine, raw, true);
             }
         }
         cluster_sync_all();                                                // nobody leaves while another reads here
@@ -465,28 +470,28 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     p.ld = (uint64_t)out_row_stride;
     p.out_dtype = (uint32_t)out_dtype;
     if (format == MX_E2M1 && p.s.s.rows == 1u && (uint64_t)p.p.s.rows * p.p.s.stages <= MXV_MOST && p.p.s.stages <= MXV_MAX_SMEM / mxv_smem(1u)) return vector_launch(p, (cudaStream_t)cuda_stream);
-    p.vec = aligned_16(out_dev) && (m == 1 || out_row_stride * size % 16 == 0);
     const uint64_t rows_s = p.s.s.rows;
     const uint64_t blocks_p = (p.p.s.rows + 127u) / 128u;
     uint32_t bn = rows_s <= 16 ? 16u : rows_s <= 32 ? 32u : rows_s <= 64 ? 64u : 128u;
     if (bn == 128u && blocks_p * ((rows_s + 255u) / 256u) >= 120u) bn = 256u;
-    const uint64_t across = (rows_s + bn - 1u) / bn, tiles = blocks_p * across;
-    if (tiles >= (1ull << 31)) return DIV_ERR_SHAPE;
-    p.tiles_p = (uint32_t)blocks_p;
-    p.tiles = (uint32_t)tiles;
-    p.split = 1;
+    const auto tiles_of = [&](uint32_t width) { return blocks_p * ((rows_s + width - 1u) / width); };
+    if (tiles_of(bn) >= (1ull << 31)) return DIV_ERR_SHAPE;
     // large products of e2m1: by pairs of CTAs, whose start and end take longer than they save with rows of less than 4096 numbers or fewer
     // than two rounds of tiles (mx_pair.cu has both sides' times; it counts rows of 128 bytes in 31 bits)
-    const uint64_t paired = (blocks_p + 1u) / 2u * across;
+    const uint64_t paired = (blocks_p + 1u) / 2u * ((rows_s + 255u) / 256u);
     if (format == MX_E2M1 && bn == 256u && p.p.s.stages >= 16u && paired >= MXP_SMS && ((mx_codes_bytes(p.p.s) | mx_codes_bytes(p.s.s)) >> 38) == 0) {
         p.tiles_p = (uint32_t)((blocks_p + 1u) / 2u);
         p.tiles = (uint32_t)paired;
+        p.split = 1;
         return mx_pair_launch(p, (cudaStream_t)cuda_stream);
     }
+    // few tiles: the sum is split, as long as a CTA keeps two stages
     uint32_t split = 1;
-    while (bn < 256u && split < 8u && tiles * split * 2u <= 160u && p.p.s.stages >= 4u * split) split *= 2u;
+    while (bn < 256u && split < 8u && tiles_of(bn) * split * 2u <= 160u && p.p.s.stages >= 4u * split) split *= 2u;
+    p.tiles_p = (uint32_t)blocks_p;
+    p.tiles = (uint32_t)tiles_of(bn);
     p.split = split;
-    const uint32_t grid = split > 1u ? (uint32_t)tiles * split : (uint32_t)(tiles < MXP_SMS ? tiles : MXP_SMS);
+    const uint32_t grid = split > 1u ? p.tiles * split : p.tiles < MXP_SMS ? p.tiles : MXP_SMS;
     return format == MX_E4M3 ? product_by_width<MX_E4M3>(bn, p, grid, (cudaStream_t)cuda_stream)
                              : product_by_width<MX_E2M1>(bn, p, grid, (cudaStream_t)cuda_stream);
 }

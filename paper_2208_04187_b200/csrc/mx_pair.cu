@@ -209,13 +209,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) mxr_arrive_first(&ctl->taken);
-            if (i < p.p.s.rows && j < p.s.s.rows) {
-                const uint64_t at = (uint64_t)i * p.ld + j;
-                const uint32_t left = p.s.s.rows - j;
-                if (p.out_dtype == DIV_BF16) mxp_row<__nv_bfloat16, 128>(static_cast<__nv_bfloat16*>(p.out) + at, left, raw, good);
-                else if (p.out_dtype == DIV_F16) mxp_row<__half, 128>(static_cast<__half*>(p.out) + at, left, raw, good);
-                else mxp_row<float, 128>(static_cast<float*>(p.out) + at, left, raw, good);
-            }
+            mxp_row_any<128>(p, i, j, 128u, raw, good);
         }
     }
     __syncwarp();

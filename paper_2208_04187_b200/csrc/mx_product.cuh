@@ -22,7 +22,6 @@ struct MxProductParams {
     uint32_t swapped;            // the lanes are columns of out
     uint32_t out_dtype;
     uint32_t split;              // CTAs of a cluster
-    uint32_t vec;                // out: rows begin at multiples of 16 bytes
 };
 struct MxCtl {
     uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES];
@@ -106,40 +105,20 @@ __device__ __forceinline__ float ld_cluster(uint32_t at) {
     return v;
 }
 
+// up to 32 numbers of a lane into a column of out
 template <typename OT>
-__device__ __forceinline__ void mxp_store_run(OT* to, const float (&v)[32], uint32_t count, bool vec) {
-#pragma unroll
-    for (uint32_t g = 0; g < 32u; g += 8u) {
-        float w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = v[g + k];
-        if (vec && g + 8u <= count) {
-            Row8<OT> r;
-            r.set(w);
-            r.store(to + g);
-        } else if (g < count) {
-            store8_any(to + g, count - g, w);
-        }
-    }
-}
-template <typename OT>
-__device__ __forceinline__ void mxp_out(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
+__device__ __forceinline__ void mxp_column(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
     if (row_p >= p.p.s.rows || row_s >= p.s.s.rows) return;
     const uint32_t count = min(n, p.s.s.rows - row_s);
-    OT* out = static_cast<OT*>(p.out);
-    if (p.swapped) {
-        OT* to = out + (uint64_t)row_s * p.ld + row_p;
+    OT* to = static_cast<OT*>(p.out) + (uint64_t)row_s * p.ld + row_p;
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if ((uint32_t)i < count) to[i * p.ld] = from_f32<OT>(v[i]);
-    } else {
-        mxp_store_run(out + (uint64_t)row_p * p.ld + row_s, v, count, p.vec && (row_s & 7u) == 0u);
-    }
+    for (int i = 0; i < 32; ++i)
+        if ((uint32_t)i < count) to[i * p.ld] = from_f32<OT>(v[i]);
 }
-__device__ __forceinline__ void mxp_out_any(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
-    if (p.out_dtype == DIV_BF16) mxp_out<__nv_bfloat16>(p, row_p, row_s, n, v);
-    else if (p.out_dtype == DIV_F16) mxp_out<__half>(p, row_p, row_s, n, v);
-    else mxp_out<float>(p, row_p, row_s, n, v);
+__device__ __forceinline__ void mxp_column_any(const MxProductParams& p, uint32_t row_p, uint32_t row_s, uint32_t n, const float (&v)[32]) {
+    if (p.out_dtype == DIV_BF16) mxp_column<__nv_bfloat16>(p, row_p, row_s, n, v);
+    else if (p.out_dtype == DIV_F16) mxp_column<__half>(p, row_p, row_s, n, v);
+    else mxp_column<float>(p, row_p, row_s, n, v);
 }
 
 // C numbers of a row of out, of which `left` are there, in 16-byte stores wherever the row begins
@@ -170,6 +149,17 @@ __device__ __forceinline__ void mxp_row(OT* to, uint32_t left, const uint32_t (&
         }
         one = next;
     }
+}
+
+// the same in out's type: numbers n of row i from column j on
+template <uint32_t C>
+__device__ __forceinline__ void mxp_row_any(const MxProductParams& p, uint32_t i, uint32_t j, uint32_t n, const uint32_t (&raw)[(C + 31u) / 32u][32], bool good) {
+    if (i >= p.p.s.rows || j >= p.s.s.rows) return;
+    const uint64_t at = (uint64_t)i * p.ld + j;
+    const uint32_t left = min(n, p.s.s.rows - j);
+    if (p.out_dtype == DIV_BF16) mxp_row<__nv_bfloat16, C>(static_cast<__nv_bfloat16*>(p.out) + at, left, raw, good);
+    else if (p.out_dtype == DIV_F16) mxp_row<__half, C>(static_cast<__half*>(p.out) + at, left, raw, good);
+    else mxp_row<float, C>(static_cast<float*>(p.out) + at, left, raw, good);
 }
 
 // mx_pair.cu: e2m1, tiles of 256 x 256 (tiles_p, tiles: of those)
