@@ -232,39 +232,44 @@ template <typename T> struct Units {
     }
     // N units from p on, of which `left` numbers are there (the rest: 0), in two steps, so that many reads can be under way together:
     // ask() reads the aligned units that they lie in, take() cuts them out.  The matrix lies between `begin` and `end`: nothing outside is
-    // read (a row's neighbours may be); what lies at its own two ends is read by take(), number by number.
+    // read (a row's neighbours may be); what lies at its own two ends ask() reads number by number.
     template <int N> static __device__ __forceinline__ bool inside(const T* p, const T* begin, const T* end) {
         const uint32_t o = offset(p);
         return p - o >= begin && p - o + (o ? N + 1 : N) * E <= end;
     }
+    template <typename F> static __device__ __forceinline__ uint4 made(F&& number_at) {        // of numbers 0 .. E-1, as words
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) {
+            const T v = number_at(i);
+            if (sizeof(T) == 4) w[i & 3u] = *reinterpret_cast<const uint32_t*>(&v);
+            else w[(i >> 1) & 3u] |= (uint32_t)*reinterpret_cast<const unsigned short*>(&v) << (16u * (i & 1u));
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
     template <int N> static __device__ __forceinline__ void ask(const T* p, const T* begin, const T* end, uint32_t left, uint4 (&a)[N + 1]) {
         const uint32_t o = offset(p);
         const uint4* at = reinterpret_cast<const uint4*>(p - o);
-        const bool in = left != 0u && inside<N>(p, begin, end);
+        const bool in = inside<N>(p, begin, end);
 #pragma unroll
         for (int u = 0; u <= N; ++u) {
             a[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (in && (u < N || o != 0u)) a[u] = at[u];
+            if (left != 0u && in && (u < N || o != 0u)) a[u] = at[u];
+        }
+        if (left != 0u && !in) {
+#pragma unroll
+            for (uint32_t u = 0; u < N; ++u) a[u] = made([&](uint32_t i) { return u * E + i < left ? p[u * E + i] : from_f32<T>(0.f); });
         }
     }
     template <int N> static __device__ __forceinline__ void take(const T* p, const T* begin, const T* end, uint32_t left, const uint4 (&a)[N + 1], uint4 (&q)[N]) {
-        const uint32_t o = offset(p);
+        const uint32_t o = inside<N>(p, begin, end) ? offset(p) : 0u;
 #pragma unroll
         for (int u = 0; u < N; ++u) q[u] = cut(a[u], a[u + 1], o);
-        if (left != 0u && (left < N * E || !inside<N>(p, begin, end))) {
-            const bool in = inside<N>(p, begin, end);
+        if (left < N * E) {
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                for (uint32_t i = 0; i < E; ++i) {
-                    if (u * E + i < left) {
-                        const T v = in ? number(q[u], i) : p[u * E + i];
-                        if (sizeof(T) == 4) w[i & 3u] = *reinterpret_cast<const uint32_t*>(&v);
-                        else w[(i >> 1) & 3u] |= (uint32_t)*reinterpret_cast<const unsigned short*>(&v) << (16u * (i & 1u));
-                    }
-                }
-                q[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (uint32_t u = 0; u < N; ++u) {
+                const uint4 whole = q[u];
+                q[u] = made([&](uint32_t i) { return u * E + i < left ? number(whole, i) : from_f32<T>(0.f); });
             }
         }
     }

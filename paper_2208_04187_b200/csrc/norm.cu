@@ -136,7 +136,7 @@ __device__ __forceinline__ void norm_out(const NormParams& p, uint32_t row, bool
 }
 
 template <typename XT, typename WT, int FMT, bool VEC, int HELD>       // HELD: pieces that a thread holds; 0: rows are read twice
-__global__ void __launch_bounds__(NORM_MAX_THREADS, !VEC && (HELD == 1 || HELD == 2) ? 2 : 1)
+__global__ void __launch_bounds__(NORM_MAX_THREADS)
 norm_forward_kernel(const __grid_constant__ NormParams p) {
     __shared__ float shared[32];
     const uint32_t per = blockDim.x / p.group, t = threadIdx.x % p.group;

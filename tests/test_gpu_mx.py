@@ -204,3 +204,34 @@ def test_large_products_of_4_bits(m, n, k, dtype):
     y = lm.mx_matmul(qa, qb, TYPES[dtype])
     assert torch.equal(y, want.to(TYPES[dtype]))
     assert torch.equal(lm.mx_matmul(qa, qb, TYPES[dtype]), y)
+
+
+def test_one_token_of_4_bits():
+    """The kernel that reads codes itself: NaN blocks, scales far apart, rows of P that end inside a CTA, in every type of out."""
+    a, b = torch.ones(1, 300), torch.ones(77, 300)
+    a[0, 32:64] *= 2.0 ** 110
+    a[0, 64:] = 0
+    b[0, 32:64] *= 2.0 ** -120
+    b[1, :32] *= 2.0 ** 127 / 64
+    b[2, 32:64] *= 2.0 ** 17
+    qb = lm.mx_quantize(b.cuda(), "e2m1")
+    y = lm.mx_matmul(lm.mx_quantize(a.cuda(), "e2m1"), qb, torch.float32).cpu()
+    assert torch.equal(y, (a.double() @ b.double().t()).float())          # (sums whose smaller term is below half a unit of the larger)
+    for dtype in TYPES.values():
+        z = lm.mx_matmul(lm.mx_quantize(torch.ones(1, 300).cuda(), "e2m1"), lm.mx_quantize(torch.ones(77, 300).cuda(), "e2m1"), dtype)
+        assert torch.equal(z, torch.full((1, 77), 300.0, dtype=dtype, device="cuda"))
+        assert torch.equal(lm.mx_matmul(lm.mx_quantize(torch.ones(77, 300).cuda(), "e2m1"), lm.mx_quantize(torch.ones(1, 300).cuda(), "e2m1"), dtype), z.t())
+    b[5, 299] = float("nan")
+    y = lm.mx_matmul(lm.mx_quantize(a.cuda(), "e2m1"), lm.mx_quantize(b.cuda(), "e2m1"), torch.float32).cpu()
+    assert y[0, 5].isnan() and int(y.isnan().sum()) == 1
+    a[0, 7] = float("inf")
+    assert lm.mx_matmul(lm.mx_quantize(a.cuda(), "e2m1"), qb, torch.float32).isnan().all()
+
+
+def test_nan_in_a_large_product_of_4_bits():
+    a, b = torch.ones(3000, 4096, device="cuda"), torch.ones(3100, 4096, device="cuda")
+    a[2999, 4095], b[3099, 0], b[128, 2000] = float("nan"), float("inf"), float("nan")
+    y = lm.mx_matmul(lm.mx_quantize(a, "e2m1"), lm.mx_quantize(b, "e2m1"), torch.float32)
+    bad = torch.zeros(3000, 3100, dtype=torch.bool, device="cuda")
+    bad[2999], bad[:, 3099], bad[:, 128] = True, True, True
+    assert torch.equal(y.isnan(), bad) and (y[~bad] == 4096).all()
