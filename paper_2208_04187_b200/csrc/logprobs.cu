@@ -6,7 +6,7 @@
 // m and log s are kept apart: their sum would lose log s next to a large m.
 //
 // Forward is bound by memory where the vocabulary is long (one reading of the logits), by the exponentials next (16 a clock and SM).  A
-// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, 4 or 8 of them under way together, and
+// cluster of 1 to 8 CTAs takes a row; a thread takes 16-byte pieces of it, LP_THREADS apart, 4 of them under way together, and
 // joins its sums with the others' in a fixed order.  Additions and products go two at a time (f32x2).
 //
 // The most probable tokens come from the same pass.  The k-th largest of the 64 maxima of the CTA's groups of 4 threads is a bound that
@@ -20,6 +20,7 @@ namespace divk {
 
 constexpr uint32_t LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_MAX_TOP = 32, LP_MAX_CLUSTER = 8;
 constexpr float LP_LOG2E = 1.4426950408889634f;
+constexpr uint32_t LP_AT_ONCE = 4;              // pieces of a thread under way together
 constexpr float LP_LEAST = -1000.f;             // exp of it is 0, and 0 times it is no NaN
 
 struct LogprobParams {
@@ -277,9 +278,10 @@ __device__ __forceinline__ void lp_rank_entries(LogprobShared& sh, uint32_t n, u
     }
 }
 
-// LP_AT_ONCE pieces of a thread are under way together: 8 where few CTAs have the device to themselves, else 4, so that 6 CTAs fit an SM
-template <typename XT, bool TOP, uint32_t LP_AT_ONCE>
-__global__ void __launch_bounds__(LP_THREADS, LP_AT_ONCE == 8 ? 2 : 6)
+// (8 pieces of a thread under way together, of 2 to 4 CTAs an SM, took longer than 4 of 6: 37 rows of 131072 bf16 with 5 alternatives 14.5
+// and 9.5 us.)
+template <typename XT, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS, 6)
 logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
     typedef Pieces<XT> P;
     __shared__ LogprobShared sh;
@@ -632,8 +634,7 @@ div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride
     if ((uint64_t)rows * split >= (1ull << 31)) return DIV_ERR_SHAPE;
     return with_type(dtype, [&](auto* t) {
         typedef std::remove_pointer_t<decltype(t)> XT;
-        auto kern = split > 1u ? (top ? logprob_forward_kernel<XT, true, 8> : logprob_forward_kernel<XT, false, 8>)
-                              : (top ? logprob_forward_kernel<XT, true, 4> : logprob_forward_kernel<XT, false, 4>);
+        auto kern = top ? logprob_forward_kernel<XT, true> : logprob_forward_kernel<XT, false>;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((uint32_t)rows * split);
         cfg.blockDim = dim3(LP_THREADS);
