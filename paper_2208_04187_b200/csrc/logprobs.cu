@@ -20,6 +20,7 @@ namespace divk {
 
 constexpr uint32_t LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_MAX_TOP = 32, LP_MAX_CLUSTER = 8;
 constexpr float LP_LOG2E = 1.4426950408889634f;
+constexpr uint32_t LP_RESIDENT = 6, LP_SMEM = 228u * 1024u;      // CTAs of an SM; its shared memory
 constexpr uint32_t LP_AT_ONCE = 4;              // pieces of a thread under way together
 constexpr float LP_LEAST = -1000.f;             // exp of it is 0, and 0 times it is no NaN
 
@@ -281,7 +282,7 @@ __device__ __forceinline__ void lp_rank_entries(LogprobShared& sh, uint32_t n, u
 // (8 pieces of a thread under way together, of 2 to 4 CTAs an SM, took longer than 4 of 6: 37 rows of 131072 bf16 with 5 alternatives 14.5
 // and 9.5 us.)
 template <typename XT, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 6)
+__global__ void __launch_bounds__(LP_THREADS, LP_RESIDENT)
 logprob_forward_kernel(const __grid_constant__ LogprobParams p) {
     typedef Pieces<XT> P;
     __shared__ LogprobShared sh;
@@ -631,7 +632,7 @@ div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride
     uint32_t split = 1;
     while (split < LP_MAX_CLUSTER && (uint64_t)rows * split < 296u && pieces >= 2ull * split * LP_THREADS) split *= 2u;
     p.split = split;
-    if ((uint64_t)rows * split >= (1ull << 31)) return DIV_ERR_SHAPE;
+    if ((uint64_t)rows * split >= (1ull << 31) - 512u) return DIV_ERR_SHAPE;
     return with_type(dtype, [&](auto* t) {
         typedef std::remove_pointer_t<decltype(t)> XT;
         auto kern = top ? logprob_forward_kernel<XT, true> : logprob_forward_kernel<XT, false>;
@@ -639,6 +640,15 @@ div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride
         cfg.gridDim = dim3((uint32_t)rows * split);
         cfg.blockDim = dim3(LP_THREADS);
         cfg.stream = (cudaStream_t)cuda_stream;
+        // Fewer CTAs than places: some SMs would get 6 while others get 2.  Shared memory that nobody uses leaves as many places as an even
+        // share takes (500 rows of 100003 bf16 37 -> 29 us, 250 of 131072 in clusters of two 25.6 -> 20.3, 500 of 2000 5.7 -> 4.7; 300 of 131072
+        // 24.9 -> 27.3).  Larger clusters need the room to be placed.
+        const uint32_t share = ((uint32_t)rows * split + 147u) / 148u;
+        if (split <= 2u && share < LP_RESIDENT && share > 1u) {
+            static SmemAllowed allowed[2];
+            cfg.dynamicSmemBytes = LP_SMEM / share - 5u * 1024u;              // (what a CTA has besides: its own 3.7 KB, the system's 1 KB)
+            if (!allowed[top ? 1 : 0]((const void*)kern, LP_SMEM / 2u)) return DIV_ERR_CUDA;
+        }
         cudaLaunchAttribute at[2];
         at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at[0].val.programmaticStreamSerializationAllowed = 1;
