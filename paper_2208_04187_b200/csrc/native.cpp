@@ -369,6 +369,10 @@ struct LogprobsFn : Function<LogprobsFn> {
 
 // ---- the calls ----
 bool wants_grad(std::initializer_list<const Tensor*> all) {
+    // (a tensor with a tangent need not ask for a gradient; past the graph its tangent would be lost, which reads as 0)
+    if (c10::AutogradState::get_tls_state().get_fw_grad_mode())
+        for (const Tensor* t : all)
+            TORCH_CHECK_NOT_IMPLEMENTED(!t->defined() || !t->_fw_grad(0).defined(), "this operator has no forward-mode derivative");
     if (!at::GradMode::is_enabled()) return false;
     for (const Tensor* t : all)
         if (t->defined() && t->requires_grad()) return true;

@@ -232,3 +232,27 @@ def test_saved_tensors_are_watched():
         z.zero_()                                       # (its quantised form alone is kept)
     dw = torch.autograd.grad(y.float().sum(), w)[0]
     assert dw.abs().sum() > 0
+
+
+def test_forward_mode_derivatives_are_refused():
+    """A tensor with a tangent need not ask for a gradient: an output without a tangent would say that the derivative is 0."""
+    forward_ad = torch.autograd.forward_ad
+    x, g, w = make(8, 64, seed=1).cuda(), make(64, seed=2).cuda(), make(16, 64, seed=3).cuda()
+    t = torch.arange(8, device="cuda")
+    calls = [lambda x, r, g, w: lm.mx_linear(x, w), lambda x, r, g, w: lm.rms_norm(x, g, r)[0], lambda x, r, g, w: lm.mx_norm_linear(x, g, w, r)[0]]
+    takes = [(0, 3), (0, 1, 2), (0, 1, 2, 3)]
+    with forward_ad.dual_level():
+        for call, which in zip(calls, takes):
+            for i in which:
+                args = [x, x, g, w]
+                args[i] = forward_ad.make_dual(args[i], torch.ones_like(args[i]))
+                for grad in (True, False):
+                    with torch.set_grad_enabled(grad), pytest.raises(NotImplementedError, match="forward-mode"):
+                        call(*args)
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        with pytest.raises(NotImplementedError, match="forward-mode"):
+            lm.token_logprobs(dual, t)
+        with torch.inference_mode():                                   # (where torch passes no tangents on either)
+            assert torch.equal(lm.token_logprobs(dual, t).logprobs, lm.token_logprobs(x, t).logprobs)
+        for call in calls:                                             # no tangent, no refusal
+            call(x, x, g, w)
