@@ -190,7 +190,8 @@ def to_division_layers(module: torch.nn.Module, fmt: str = "e4m3") -> torch.nn.M
             new.weight, new.bias = child.weight, child.bias
             setattr(module, name, new.train(child.training))
         elif type(child) is torch.nn.RMSNorm and len(child.normalized_shape) == 1 and child.weight is not None:
-            eps = torch.finfo(child.weight.dtype).eps if child.eps is None else child.eps
+            # (torch's default: the epsilon of the type that it computes in, float32 for the 16-bit types)
+            eps = torch.finfo(torch.float32).eps if child.eps is None else child.eps
             new = DivisionRMSNorm(child.normalized_shape[0], eps, device="meta")
             new.weight = child.weight
             setattr(module, name, new.train(child.training))

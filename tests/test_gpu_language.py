@@ -256,3 +256,15 @@ def test_forward_mode_derivatives_are_refused():
             assert torch.equal(lm.token_logprobs(dual, t).logprobs, lm.token_logprobs(x, t).logprobs)
         for call in calls:                                             # no tangent, no refusal
             call(x, x, g, w)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_a_replaced_norm_gives_what_torchs_gave(dtype):
+    """Without an epsilon of its own, on rows so small that it decides."""
+    norm = torch.nn.RMSNorm(64, device="cuda", dtype=dtype)
+    x = make(5, 64, seed=1, scale=0.01, dtype=dtype).cuda()
+    want = norm(x)
+    got = lm.to_division_layers(torch.nn.Sequential(norm))[0](x)
+    # both: a sum of 64 and a handful of operations in 32 bits, then half a step
+    size = want.double().abs()
+    assert ((got.double() - want.double()).abs() <= 2 * (torch.finfo(dtype).eps / 2 + 40 * 2.0 ** -24) * (1 + 2.0 ** -8) * size).all()

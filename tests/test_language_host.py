@@ -150,3 +150,15 @@ def test_layers_are_replaced_with_their_parameters():
     assert lm.to_division_layers(net, "e2m1") is net
     assert [type(m).__name__ for m in net.modules()] == ["Sequential", "DivisionRMSNorm", "DivisionLinear", "Sequential", "DivisionLinear", "LayerNorm"]
     assert all(a is b for a, b in zip(kept, net.parameters())) and net[1].fmt == "e2m1" and net[0].eps == torch.finfo(torch.float32).eps
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_a_norm_without_an_epsilon_keeps_torchs(dtype):
+    """Rows so small that the epsilon decides: what the replaced norm adds gives torch's own output."""
+    norm = torch.nn.RMSNorm(64, dtype=dtype)
+    x = (0.01 * torch.randn(5, 64, generator=torch.Generator().manual_seed(1))).to(dtype)
+    new = lm.to_division_layers(torch.nn.Sequential(norm))[0]
+    f = x.double()
+    want = f / (f.square().mean(1, keepdim=True) + new.eps).sqrt()
+    # torch rounds in 32 bits on its way (a handful of times), then to dtype
+    assert ((norm(x).double() - want).abs() <= (torch.finfo(dtype).eps / 2 + 40 * 2.0 ** -24) * want.abs()).all()
