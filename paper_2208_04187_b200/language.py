@@ -182,19 +182,33 @@ class DivisionNormLinear(torch.nn.Module):
 
 
 def to_division_layers(module: torch.nn.Module, fmt: str = "e4m3") -> torch.nn.Module:
-    """Replace every nn.Linear in `module` by DivisionLinear and every nn.RMSNorm over one dimension by DivisionRMSNorm, with their
-    parameters (in place; returns the module)."""
-    for name, child in list(module.named_children()):
+    """Replace every nn.Linear below `module` by DivisionLinear and every nn.RMSNorm over one dimension by DivisionRMSNorm, with their
+    parameters (in place; returns the module).  A layer that is used in several places is replaced by one in all of them; hooks of a
+    replaced layer are not carried over."""
+    made = {}                                       # what has been seen -> what stands in its place
+
+    def replaced(child):
+        if child in made:
+            return made[child]
+        new = child
         if type(child) is torch.nn.Linear:
             new = DivisionLinear(child.in_features, child.out_features, child.bias is not None, fmt, device="meta")
             new.weight, new.bias = child.weight, child.bias
-            setattr(module, name, new.train(child.training))
         elif type(child) is torch.nn.RMSNorm and len(child.normalized_shape) == 1 and child.weight is not None:
             # (torch's default: the epsilon of the type that it computes in, float32 for the 16-bit types)
             eps = torch.finfo(torch.float32).eps if child.eps is None else child.eps
             new = DivisionRMSNorm(child.normalized_shape[0], eps, device="meta")
             new.weight = child.weight
-            setattr(module, name, new.train(child.training))
-        else:
-            to_division_layers(child, fmt)
+        made[child] = new.train(child.training) if new is not child else child
+        if new is child:
+            below(child)
+        return made[child]
+
+    def below(parent):
+        # (named_children names a child once, however often it is used)
+        for name, child in list(parent._modules.items()):
+            if child is not None and replaced(child) is not child:
+                setattr(parent, name, made[child])
+
+    below(module)
     return module

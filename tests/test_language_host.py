@@ -162,3 +162,21 @@ def test_a_norm_without_an_epsilon_keeps_torchs(dtype):
     want = f / (f.square().mean(1, keepdim=True) + new.eps).sqrt()
     # torch rounds in 32 bits on its way (a handful of times), then to dtype
     assert ((norm(x).double() - want).abs() <= (torch.finfo(dtype).eps / 2 + 40 * 2.0 ** -24) * want.abs()).all()
+
+
+def test_a_layer_used_twice_is_replaced_in_both_places():
+    class Net(torch.nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.a = torch.nn.Linear(4, 4)
+            self.b = self.a
+            self.inner = torch.nn.Sequential(self.a, torch.nn.RMSNorm(4))
+            self.again = self.inner
+            self.none = None
+            self.register_module("empty", None)
+    net = Net()
+    w = net.a.weight
+    lm.to_division_layers(net)
+    assert type(net.a) is lm.DivisionLinear and net.b is net.a and net.inner[0] is net.a and net.again is net.inner
+    assert type(net.inner[1]) is lm.DivisionRMSNorm and net.a.weight is w and net.empty is None
+    assert not any(type(m) in (torch.nn.Linear, torch.nn.RMSNorm) for m in net.modules())
