@@ -386,10 +386,19 @@ div_status div_mx_dequantize(const void* blob_dev, size_t blob_bytes, int64_t ro
 
 /*
  * out (m x n) = A * B^T from two blobs by rows with the same format: A is m x k, B is n x k.  Products and sums in 32 bits,
- * rounded to out_dtype once.  (Should a bounded wait inside the kernel run out, its part of out is NaN.)
+ * rounded to out_dtype once.  (Should a bounded wait inside the kernel run out, what it has not summed by then is NaN.)
  */
 div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
                          void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream);
+/*
+ * Test hook for the bounded waits of div_mx_matmul: runs the kernel that it would run, but CTA `cta` never gets the codes of A or B of the stage
+ * number `copy` that it asks for, with `timeout_ns` (1 ns to 100 ms) as the limit of every wait.  The kernel must give up, write NaN for
+ * what this CTA has not summed by then, and return.  DIV_ERR_PARAM for the kernel that
+ * waits for nothing (one row of e2m1).
+ */
+div_status div_debug_mx_matmul_starved(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
+                                       void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream, uint32_t cta, uint32_t copy,
+                                       uint64_t timeout_ns);
 
 /*
  * Root-mean-square normalisation with the residual's addition.

@@ -37,7 +37,7 @@ EXPORTED_SYMBOLS = (
     "div_mask_bytes", "div_relu_forward", "div_dropout_forward", "div_mask_backward",
     "div_planegroup_bytes", "div_planegroup_compress", "div_planegroup_decompress", "div_planegroup_plan_query",
     "div_read_device_status", "div_status_string",
-    "div_mx_bytes", "div_mx_quantize", "div_mx_dequantize", "div_mx_matmul",
+    "div_mx_bytes", "div_mx_quantize", "div_mx_dequantize", "div_mx_matmul", "div_debug_mx_matmul_starved",
     "div_rms_norm_forward", "div_rms_norm_workspace", "div_rms_norm_backward",
     "div_token_logprobs_forward", "div_token_logprobs_backward",
 )
@@ -142,6 +142,8 @@ def lib() -> ctypes.CDLL:
         L.div_mx_dequantize.restype = c_int32
         L.div_mx_matmul.argtypes = [c_void_p, c_size_t, c_void_p, c_size_t, c_int64, c_int64, c_int64, c_int32, c_void_p, c_int64, c_int32, c_void_p]
         L.div_mx_matmul.restype = c_int32
+        L.div_debug_mx_matmul_starved.argtypes = L.div_mx_matmul.argtypes + [c_uint32, c_uint32, c_uint64]
+        L.div_debug_mx_matmul_starved.restype = c_int32
         L.div_rms_norm_forward.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_int64, c_int64, c_int32, c_float, c_void_p,
                                            c_void_p, c_void_p, c_size_t, c_int32, c_void_p, c_void_p]
         L.div_rms_norm_forward.restype = c_int32

@@ -15,8 +15,8 @@
 // in its shared memory, and takes a share of the columns, which it adds up over the cluster in the order of the ranks (the result
 // does not depend on timing).
 //
-// Every wait is bounded (MXP_LIMIT_NS): a CTA that gives up waits for its copies, gives its tensor memory back, and
-// writes NaN for its tile.
+// Every wait is bounded (MXP_LIMIT_NS): a CTA that gives up waits for its copies and its products (bounded too), gives its tensor memory back, and
+// writes NaN for the tiles that it has not summed; in a cluster NaN goes into the ring once no copy can land there any more.
 #include "mx_product.cuh"
 
 namespace divk {
@@ -87,7 +87,8 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
         }
         mbar_init(&ctl->done, 1);
         mbar_init(&ctl->taken, 4u * T::HALVES);
-        ctl->failed = 0;
+        mbar_init(&ctl->last, 1);
+        ctl->failed = ctl->landed = 0;
         fence_barrier_init();
         fence_proxy_async();
     }
@@ -101,6 +102,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
     if (warp == MXP_PRODUCER && lane == 0) {
         uint32_t asked = 0;
         bool ok = true;
+        const uint32_t starved = blockIdx.x == p.starved_cta ? p.starved_copy : 0xFFFFFFFFu;
         for (uint32_t tile = first; tile < p.tiles && ok; tile += step) {
             const uint32_t tp = tile % p.tiles_p, s0 = tile / p.tiles_p * BN;
             const uint32_t hp = mx_tile_rows(p.p.s, tp) * 128u;
@@ -124,14 +126,14 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             const unsigned char* scales_p = p.p.scales + (uint64_t)tp * all * T::SCALES;
             for (uint32_t k = k0; k < k1; ++k, ++asked) {
                 const uint32_t slot = asked % T::STAGES, turn = asked / T::STAGES;
-                if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl)) {
+                if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl, p.limit_ns)) {
                     ok = false;
                     break;
                 }
                 unsigned char* at = ring + slot * T::STAGE_BYTES;
                 uint64_t* bar = &ctl->full[slot];
                 mbar_arrive_expect_tx(bar, bytes);
-                bulk_load(at, from_p + (uint64_t)k * hp, hp, bar);
+                if (asked != starved) bulk_load(at, from_p + (uint64_t)k * hp, hp, bar);
                 bulk_load(at + T::P_CODES + T::S_CODES, scales_p + (uint64_t)k * T::SCALES, T::SCALES, bar);
 #pragma unroll
                 for (uint32_t b = 0; b < T::S_BLOCKS; ++b) {
@@ -143,7 +145,9 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
         // no copy may land after the CTA has gone, whoever gave up.  (Slots of earlier fills were handed back full.)
         const uint64_t t0 = now_ns();
         for (uint32_t i = asked > T::STAGES ? asked - T::STAGES : 0u; i < asked; ++i)
-            while (!mbar_try_wait(&ctl->full[i % T::STAGES], (i / T::STAGES) & 1u) && now_ns() - t0 < MXP_LIMIT_NS) {}
+            mxp_wait_out(&ctl->full[i % T::STAGES], (i / T::STAGES) & 1u, t0, p.limit_ns);
+        __threadfence_block();
+        *(volatile uint32_t*)&ctl->landed = 1u;
     } else if (warp == MXP_ISSUER && lane == 0) {
         // dense, both operands of one type, scales with 8 bits of exponent, BN columns, 128 lanes
         const uint32_t type = FMT == MX_E2M1 ? 1u : 0u;
@@ -152,14 +156,14 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
         uint32_t n = 0, made = 0;
         bool ok = true;
         for (uint32_t tile = first; tile < p.tiles && ok; tile += step, ++made) {
-            if (made > 0u && !mxp_wait(&ctl->taken, (made - 1u) & 1u, ctl)) {
+            if (made > 0u && !mxp_wait(&ctl->taken, (made - 1u) & 1u, ctl, p.limit_ns)) {
                 ok = false;
                 break;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (uint32_t k = k0; k < k1; ++k, ++n) {
                 const uint32_t slot = n % T::STAGES;
-                if (!mxp_wait(&ctl->full[slot], (n / T::STAGES) & 1u, ctl)) {
+                if (!mxp_wait(&ctl->full[slot], (n / T::STAGES) & 1u, ctl, p.limit_ns)) {
                     ok = false;
                     break;
                 }
@@ -184,7 +188,10 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             }
             mxp_commit(&ctl->done);
         }
-        if (!ok && made > 0u) mxp_wait(&ctl->done, (made - 1u) & 1u, ctl);      // (what has been issued ends before the tensor memory goes)
+        if (!ok) {                                                              // (what has been issued ends before the tensor memory goes)
+            mxp_commit(&ctl->last);
+            mxp_wait_out(&ctl->last, 0u, now_ns(), p.limit_ns);
+        }
     } else if (warp < 4u * T::HALVES) {
         // ---- the way out: a warp has a quarter of the lanes, and all columns or half of them ----
         const uint32_t row = (warp & 3u) * 32u + lane, c0 = (warp >> 2) * T::MINE;
@@ -192,7 +199,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
         uint32_t made = 0;
         for (uint32_t tile = first; tile < p.tiles; tile += step, ++made) {
             const uint32_t p0 = tile % p.tiles_p * 128u, s0 = tile / p.tiles_p * BN;
-            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl));
+            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl, p.limit_ns));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             good = good && !*(volatile uint32_t*)&ctl->failed;
             uint32_t raw[(T::MINE + 31u) / 32u][32];
@@ -205,6 +212,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl->taken);
+            if (!good && p.split > 1u) mxp_wait_word(&ctl->landed, 0u, p.limit_ns);
             if (p.split == 1u && !p.swapped) {
                 mxp_row_any<T::MINE>(p, p0 + row, s0 + c0, T::MINE, raw, good);
                 continue;
@@ -441,12 +449,9 @@ div_status product_by_width(uint32_t bn, const MxProductParams& p, uint32_t grid
     return product_launch<FMT, 256>(p, grid, st);
 }
 
-}  // namespace
-
-extern "C" {
-
-div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
-                         void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream) {
+// (p: the limits of waits are set)
+div_status product(MxProductParams p, bool starved, const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
+                   void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream) {
     if (!a_dev || !b_dev || !out_dev) return DIV_ERR_NULL;
     if (!lm_size_ok(m) || !lm_size_ok(n) || !lm_size_ok(k) || (m > 1 && out_row_stride < n)) return DIV_ERR_SHAPE;
     if (!lm_dtype_ok(out_dtype) || !mx_format_ok(format)) return DIV_ERR_PARAM;
@@ -461,7 +466,6 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     b.codes = (const unsigned char*)b_dev;
     b.scales = b.codes + mx_scales_at(b.s);
 
-    MxProductParams p;
     const bool swapped = m < n && m <= 64;
     p.p = swapped ? b : a;
     p.s = swapped ? a : b;
@@ -469,7 +473,8 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     p.out = out_dev;
     p.ld = (uint64_t)out_row_stride;
     p.out_dtype = (uint32_t)out_dtype;
-    if (format == MX_E2M1 && p.s.s.rows == 1u && (uint64_t)p.p.s.rows * p.p.s.stages <= MXV_MOST && p.p.s.stages <= MXV_MAX_SMEM / mxv_smem(1u)) return vector_launch(p, (cudaStream_t)cuda_stream);
+    if (format == MX_E2M1 && p.s.s.rows == 1u && (uint64_t)p.p.s.rows * p.p.s.stages <= MXV_MOST && p.p.s.stages <= MXV_MAX_SMEM / mxv_smem(1u))
+        return starved ? DIV_ERR_PARAM : vector_launch(p, (cudaStream_t)cuda_stream);
     const uint64_t rows_s = p.s.s.rows;
     const uint64_t blocks_p = (p.p.s.rows + 127u) / 128u;
     uint32_t bn = rows_s <= 16 ? 16u : rows_s <= 32 ? 32u : rows_s <= 64 ? 64u : 128u;
@@ -494,6 +499,26 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
     const uint32_t grid = split > 1u ? p.tiles * split : p.tiles < MXP_SMS ? p.tiles : MXP_SMS;
     return format == MX_E4M3 ? product_by_width<MX_E4M3>(bn, p, grid, (cudaStream_t)cuda_stream)
                              : product_by_width<MX_E2M1>(bn, p, grid, (cudaStream_t)cuda_stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
+                         void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream) {
+    return product(MxProductParams(), false, a_dev, a_bytes, b_dev, b_bytes, m, n, k, format, out_dev, out_row_stride, out_dtype, cuda_stream);
+}
+
+div_status div_debug_mx_matmul_starved(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,
+                                       void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream, uint32_t cta, uint32_t copy,
+                                       uint64_t timeout_ns) {
+    if (timeout_ns == 0 || timeout_ns > 100000000ull) return DIV_ERR_PARAM;
+    MxProductParams p;
+    p.limit_ns = timeout_ns;
+    p.starved_cta = cta;
+    p.starved_copy = copy;
+    return product(p, true, a_dev, a_bytes, b_dev, b_bytes, m, n, k, format, out_dev, out_row_stride, out_dtype, cuda_stream);
 }
 
 }  // extern "C"

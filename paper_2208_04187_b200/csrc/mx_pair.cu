@@ -82,7 +82,9 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         }
         mbar_init(&ctl->done, 1);
         mbar_init(&ctl->taken, 16);
+        mbar_init(&ctl->last, 1);
         ctl->failed = 0;
+        ctl->asked = 0xFFFFFFFFu;
         fence_barrier_init();
         fence_proxy_async();
     }
@@ -100,6 +102,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         const uint32_t blocks_p = (p.p.s.rows + 127u) / 128u, blocks_s = (p.s.s.rows + 127u) / 128u;
         uint32_t asked = 0;
         bool ok = true;
+        const uint32_t starved = blockIdx.x == p.starved_cta ? p.starved_copy : 0xFFFFFFFFu;
         for (uint32_t tile = first; tile < p.tiles && ok; tile += step) {
             const uint32_t bp = tile % p.tiles_p * 2u + half, bs = tile / p.tiles_p * 2u;
             const uint32_t mine = bp < blocks_p ? bp : 0u, own = bs + half < blocks_s ? bs + half : 0u, other = bs + 1u < blocks_s ? bs + 1u : 0u;
@@ -110,7 +113,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
             const unsigned char* z1 = p.s.scales + (uint64_t)other * all * MXR_SCALES;
             for (uint32_t k = 0; k < all; ++k, ++asked) {
                 const uint32_t slot = asked % MXR_STAGES, turn = asked / MXR_STAGES;
-                if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl)) {
+                if (turn > 0u && !mxp_wait(&ctl->empty[slot], (turn - 1u) & 1u, ctl, p.limit_ns)) {
                     ok = false;
                     break;
                 }
@@ -120,7 +123,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
                 bulk_load(sc + MXR_SCALES, z0 + (uint64_t)k * MXR_SCALES, MXR_SCALES, &ctl->scaled[slot]);
                 bulk_load(sc + 2u * MXR_SCALES, z1 + (uint64_t)k * MXR_SCALES, MXR_SCALES, &ctl->scaled[slot]);
                 if (half == 0u) mbar_arrive_expect_tx(&ctl->full[slot], 4u * MXR_CODES);
-                mxr_box(at, &g.codes_p, yp + k * hp, &ctl->full[slot]);
+                if (asked != starved) mxr_box(at, &g.codes_p, yp + k * hp, &ctl->full[slot]);
                 mxr_box(at + MXR_CODES, &g.codes_s, ys + k * hs, &ctl->full[slot]);
             }
         }
@@ -128,8 +131,19 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         // counted at the first, and both leave together.)
         const uint64_t t0 = now_ns();
         for (uint32_t i = asked > MXR_STAGES ? asked - MXR_STAGES : 0u; i < asked; ++i) {
-            while (!mbar_try_wait(&ctl->scaled[i % MXR_STAGES], (i / MXR_STAGES) & 1u) && now_ns() - t0 < MXP_LIMIT_NS) {}
-            while (half == 0u && !mbar_try_wait(&ctl->full[i % MXR_STAGES], (i / MXR_STAGES) & 1u) && now_ns() - t0 < MXP_LIMIT_NS) {}
+            mxp_wait_out(&ctl->scaled[i % MXR_STAGES], (i / MXR_STAGES) & 1u, t0, p.limit_ns);
+            if (half == 0u) mxp_wait_out(&ctl->full[i % MXR_STAGES], (i / MXR_STAGES) & 1u, t0, p.limit_ns);
+        }
+        if (half != 0u) {
+            asm volatile("st.release.cluster.shared::cluster.u32 [%0], %1;" ::"r"(cluster_at(smem_u32(&ctl->asked), 0u)), "r"(asked) : "memory");
+        } else if (!ok) {
+            // stages that the second CTA alone has asked for: its codes are on their way, and complete a fill once they are expected
+            const uint32_t other = mxp_wait_word(&ctl->asked, 0xFFFFFFFFu, p.limit_ns);
+            const uint64_t t1 = now_ns();
+            for (uint32_t i = asked; i < other && other != 0xFFFFFFFFu; ++i) {
+                mbar_arrive_expect_tx(&ctl->full[i % MXR_STAGES], 2u * MXR_CODES);
+                mxp_wait_out(&ctl->full[i % MXR_STAGES], (i / MXR_STAGES) & 1u, t1, p.limit_ns);
+            }
         }
     } else if (warp == MXP_ISSUER && lane == 0 && half == 0u) {
         // dense, both operands e2m1, scales with 8 bits of exponent, 256 columns, 128 lanes of each CTA
@@ -137,14 +151,14 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         uint32_t n = 0, made = 0;
         bool ok = true;
         for (uint32_t tile = first; tile < p.tiles && ok; tile += step, ++made) {
-            if (made > 0u && !mxp_wait_cluster(&ctl->taken, (made - 1u) & 1u, ctl)) {
+            if (made > 0u && !mxp_wait_cluster(&ctl->taken, (made - 1u) & 1u, ctl, p.limit_ns)) {
                 ok = false;
                 break;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (uint32_t k = 0; k < all; ++k, ++n) {
                 const uint32_t slot = n % MXR_STAGES, turn = (n / MXR_STAGES) & 1u;
-                if (!mxp_wait_cluster(&ctl->full[slot], turn, ctl) || !mxp_wait_cluster(&ctl->ready[slot], turn, ctl)) {
+                if (!mxp_wait_cluster(&ctl->full[slot], turn, ctl, p.limit_ns) || !mxp_wait_cluster(&ctl->ready[slot], turn, ctl, p.limit_ns)) {
                     ok = false;
                     break;
                 }
@@ -161,7 +175,10 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
             }
             mxr_commit(&ctl->done);
         }
-        if (!ok && made > 0u) mxp_wait(&ctl->done, (made - 1u) & 1u, ctl);      // (what has been issued ends before the tensor memory goes)
+        if (!ok) {                                                              // (what has been issued ends before the tensor memory goes)
+            mxr_commit(&ctl->last);
+            mxp_wait_out(&ctl->last, 0u, now_ns(), p.limit_ns);
+        }
     } else if (warp >= MXR_SCALERS) {
         // ---- scales: lane l of a quarter holds those of rows l, l + 32, l + 64, l + 96, 4 bytes each, in 4 columns ----
         const uint32_t mine = (warp & 3u) << 21;
@@ -170,7 +187,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         for (uint32_t tile = first; tile < p.tiles && ok; tile += step) {
             for (uint32_t k = 0; k < all; ++k, ++n) {
                 const uint32_t slot = n % MXR_STAGES;
-                ok = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->scaled[slot], (n / MXR_STAGES) & 1u, ctl));
+                ok = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->scaled[slot], (n / MXR_STAGES) & 1u, ctl, p.limit_ns));
                 if (!ok) break;
                 const unsigned char* sc = ring + slot * MXR_STAGE_BYTES + 2u * MXR_CODES + lane * 16u;
                 const uint32_t cp = mine + scales0 + slot * MXR_COLUMNS, cs = cp + 4u * MXR_ATOMS;
@@ -199,7 +216,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         uint32_t made = 0;
         for (uint32_t tile = first; tile < p.tiles; tile += step, ++made) {
             const uint32_t i = (tile % p.tiles_p * 2u + half) * 128u + row, j = tile / p.tiles_p * 256u + c0;
-            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl));
+            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl, p.limit_ns));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             good = good && !*(volatile uint32_t*)&ctl->failed;
             uint32_t raw[4][32];

@@ -22,12 +22,17 @@ struct MxProductParams {
     uint32_t swapped;            // the lanes are columns of out
     uint32_t out_dtype;
     uint32_t split;              // CTAs of a cluster
+    uint64_t limit_ns = MXP_LIMIT_NS;      // of every wait
+    uint32_t starved_cta = 0xFFFFFFFFu, starved_copy = 0u;      // (a test's: this CTA never gets the codes of that stage, counted over all that it asks for)
 };
 struct MxCtl {
     uint64_t full[MXP_MAX_STAGES], empty[MXP_MAX_STAGES];
     uint64_t scaled[MXP_MAX_STAGES], ready[MXP_MAX_STAGES];      // pairs: scales are in shared memory, and in tensor memory
     uint64_t done, taken;        // done: a tile is summed; taken: it is in registers
+    uint64_t last;               // what a giving-up issuer has issued is through
     uint32_t tmem, failed;
+    uint32_t landed;             // (split sums) no copy is on its way any more
+    uint32_t asked;              // (pairs) stages that the second CTA has asked for in all, told to the first
 };
 
 // shared-memory matrix descriptor: start, stride between groups of 8 rows; version 1 of the layout
@@ -67,24 +72,36 @@ __device__ __forceinline__ bool mxp_try_wait_cluster(uint64_t* bar, uint32_t par
         : "memory");
     return ok != 0;
 }
-// waits for a phase, at most MXP_LIMIT_NS, and not once another thread of the CTA has given up
+// waits for a phase, at most limit_ns, and not once another thread of the CTA has given up
 template <bool CLUSTER>
-__device__ __forceinline__ bool mxp_wait_for(uint64_t* bar, uint32_t parity, MxCtl* ctl) {
+__device__ __forceinline__ bool mxp_wait_for(uint64_t* bar, uint32_t parity, MxCtl* ctl, uint64_t limit_ns) {
     uint64_t t0 = 0;
     for (uint32_t polls = 1;; ++polls) {
         if (CLUSTER ? mxp_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
         if ((polls & 63u) == 0u) {                         // (reading the timer takes longer than most waits)
             const uint64_t t = now_ns();
             if (t0 == 0u) t0 = t;
-            if (*(volatile uint32_t*)&ctl->failed || t - t0 > MXP_LIMIT_NS) {
+            if (*(volatile uint32_t*)&ctl->failed || t - t0 > limit_ns) {
                 *(volatile uint32_t*)&ctl->failed = 1u;
                 return false;
             }
         }
     }
 }
-__device__ __forceinline__ bool mxp_wait(uint64_t* bar, uint32_t parity, MxCtl* ctl) { return mxp_wait_for<false>(bar, parity, ctl); }
-__device__ __forceinline__ bool mxp_wait_cluster(uint64_t* bar, uint32_t parity, MxCtl* ctl) { return mxp_wait_for<true>(bar, parity, ctl); }
+__device__ __forceinline__ bool mxp_wait(uint64_t* bar, uint32_t parity, MxCtl* ctl, uint64_t limit_ns) { return mxp_wait_for<false>(bar, parity, ctl, limit_ns); }
+__device__ __forceinline__ bool mxp_wait_cluster(uint64_t* bar, uint32_t parity, MxCtl* ctl, uint64_t limit_ns) { return mxp_wait_for<true>(bar, parity, ctl, limit_ns); }
+// On the way out, for what a CTA has started and must not leave behind (copies, products): whoever has given up.
+__device__ __forceinline__ void mxp_wait_out(uint64_t* bar, uint32_t parity, uint64_t t0, uint64_t limit_ns) {
+    while (!mbar_try_wait(bar, parity) && now_ns() - t0 < limit_ns) {}
+}
+// Waits until a word is no longer `until`, three limits at most: another thread's last wait, and what it waits for on its way out
+__device__ __forceinline__ uint32_t mxp_wait_word(const uint32_t* word, uint32_t until, uint64_t limit_ns) {
+    const uint64_t t0 = now_ns();
+    uint32_t v;
+    while ((v = *(const volatile uint32_t*)word) == until && now_ns() - t0 < 3u * limit_ns) {}
+    __threadfence_block();
+    return v;
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

@@ -235,3 +235,35 @@ def test_nan_in_a_large_product_of_4_bits():
     bad = torch.zeros(3000, 3100, dtype=torch.bool, device="cuda")
     bad[2999], bad[:, 3099], bad[:, 128] = True, True, True
     assert torch.equal(y.isnan(), bad) and (y[~bad] == 4096).all()
+
+
+# (m, n, k, format, width of a tile, CTAs of a cluster, the lanes are columns of out, CTAs of the launch); width 512: pairs
+STARVED = [(40, 1000, 4096, "e4m3", 64, 8, True, 64), (9, 700, 2000, "e2m1", 16, 4, True, 24), (300, 200, 4096, "e4m3", 128, 8, False, 48),
+           (300, 200, 4096, "e2m1", 128, 8, False, 48), (1280, 2304, 700, "e4m3", 128, 1, False, 148), (33, 20000, 300, "e2m1", 64, 1, True, 148),
+           (2300, 2200, 1100, "e4m3", 256, 1, False, 148), (2300, 2200, 1100, "e2m1", 256, 1, False, 148), (3000, 3100, 4096, "e2m1", 512, 2, False, 148)]
+
+
+def starved(qa, qb, m, n, k, fmt, cta, copy):
+    out = torch.full((m, n), 7.0, device="cuda")
+    st = binding.lib().div_debug_mx_matmul_starved(qa.blob.data_ptr(), qa.blob.numel(), qb.blob.data_ptr(), qb.blob.numel(), m, n, k, binding.MX_FORMATS[fmt],
+                                                   out.data_ptr(), n, binding.DIV_F32, binding.current_stream_handle(), cta, copy, 2_000_000)
+    assert st == binding.DIV_OK
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("m, n, k, fmt, width, split, swapped, grid", STARVED)
+@pytest.mark.parametrize("cta, copy", [(0, 0), (1, 1), (6, 3)])
+def test_a_product_whose_wait_cannot_end_returns(m, n, k, fmt, width, split, swapped, grid, cta, copy):
+    """Failure detection without a fault: a CTA waits for codes that nobody asks for, its 2 ms limit runs out, it waits for what it has started and
+    leaves.  Where a cluster shares a sum, all of that tile is NaN, whatever copies were on their way; the next call finds everything in order."""
+    qa, qb = lm.mx_quantize(matrix(m, k, "bf16", 1, 0.5).cuda(), fmt), lm.mx_quantize(matrix(n, k, "bf16", 2, 0.5).cuda(), fmt)
+    want = lm.mx_matmul(qa, qb, torch.float32)
+    out = starved(qa, qb, m, n, k, fmt, cta, copy)
+    run = -(-k // (128 if fmt == "e4m3" else 256)) // split               # stages of a CTA, at least
+    if width < 256 and split > 1 and copy < run:
+        p = cta // split % -(-(n if swapped else m) // 128) * 128
+        part = (out.t() if swapped else out)[p:p + 128]
+        s = cta // split // -(-(n if swapped else m) // 128) * width
+        assert part[:, s:s + width].isnan().all()
+    assert torch.equal(lm.mx_matmul(qa, qb, torch.float32), want)

@@ -180,3 +180,12 @@ def test_a_layer_used_twice_is_replaced_in_both_places():
     assert type(net.a) is lm.DivisionLinear and net.b is net.a and net.inner[0] is net.a and net.again is net.inner
     assert type(net.inner[1]) is lm.DivisionRMSNorm and net.a.weight is w and net.empty is None
     assert not any(type(m) in (torch.nn.Linear, torch.nn.RMSNorm) for m in net.modules())
+
+
+def test_refusals_of_the_starved_product():
+    m = binding.lib().div_debug_mx_matmul_starved
+    big = 1 << 30
+    for limit in (0, 100_000_001):
+        assert m(256, big, 256, big, 4, 4, 32, 0, 256, 4, 0, None, 0, 0, limit) == binding.DIV_ERR_PARAM
+    assert m(None, big, 256, big, 4, 4, 32, 0, 256, 4, 0, None, 0, 0, 1) == binding.DIV_ERR_NULL
+    assert m(256, big, 256, big, 1, 4, 32, 1, 256, 4, 0, None, 0, 0, 1) == binding.DIV_ERR_PARAM      # one row of 4 bits: nothing is waited for
