@@ -392,8 +392,8 @@ div_status div_mx_matmul(const void* a_dev, size_t a_bytes, const void* b_dev, s
                          void* out_dev, int64_t out_row_stride, int32_t out_dtype, void* cuda_stream);
 /*
  * Test hook for the bounded waits of div_mx_matmul: runs the kernel that it would run, but CTA `cta` never gets the codes of A or B of the stage
- * number `copy` that it asks for, with `timeout_ns` (1 ns to 100 ms) as the limit of every wait.  The kernel must give up, write NaN for
- * what this CTA has not summed by then, and return.  DIV_ERR_PARAM for the kernel that
+ * number `copy` that it asks for, with `timeout_ns` (1 ns to 100 ms) as the limit of every wait.  The kernel must give up, write NaN for the
+ * tiles that this CTA and its cluster have not summed by then, and return; the rest of out is as ever.  DIV_ERR_PARAM for the kernel that
  * waits for nothing (one row of e2m1).
  */
 div_status div_debug_mx_matmul_starved(const void* a_dev, size_t a_bytes, const void* b_dev, size_t b_bytes, int64_t m, int64_t n, int64_t k, int32_t format,

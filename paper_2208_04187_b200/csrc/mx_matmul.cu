@@ -16,7 +16,8 @@
 // does not depend on timing).
 //
 // Every wait is bounded (MXP_LIMIT_NS): a CTA that gives up waits for its copies and its products (bounded too), gives its tensor memory back, and
-// writes NaN for the tiles that it has not summed; in a cluster NaN goes into the ring once no copy can land there any more.
+// writes NaN for the tiles that it has not summed.  A tile is taken for summed when the commit behind its last product has come and in no
+// other way; in a cluster NaN goes into the ring once no copy can land there any more.
 #include "mx_product.cuh"
 
 namespace divk {
@@ -186,7 +187,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
                 }
                 mxp_commit(&ctl->empty[slot]);
             }
-            mxp_commit(&ctl->done);
+            if (ok) mxp_commit(&ctl->done);
         }
         if (!ok) {                                                              // (what has been issued ends before the tensor memory goes)
             mxp_commit(&ctl->last);
@@ -197,11 +198,11 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
         const uint32_t row = (warp & 3u) * 32u + lane, c0 = (warp >> 2) * T::MINE;
         const uint32_t from = tmem + ((warp & 3u) << 21) + c0;          // its first lane in the upper half of the address
         uint32_t made = 0;
+        bool good = true;                   // (for good: behind a phase that never ended, the next one's parity reads as ended)
         for (uint32_t tile = first; tile < p.tiles; tile += step, ++made) {
             const uint32_t p0 = tile % p.tiles_p * 128u, s0 = tile / p.tiles_p * BN;
-            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl, p.limit_ns));
+            good = good && __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl, p.limit_ns));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            good = good && !*(volatile uint32_t*)&ctl->failed;
             uint32_t raw[(T::MINE + 31u) / 32u][32];
             __syncwarp();
 #pragma unroll
@@ -211,7 +212,7 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl->taken);
+            if (lane == 0 && good) mbar_arrive(&ctl->taken);          // (the next tile waits for those who have read this one, and for them alone)
             if (!good && p.split > 1u) mxp_wait_word(&ctl->landed, 0u, p.limit_ns);
             if (p.split == 1u && !p.swapped) {
                 mxp_row_any<T::MINE>(p, p0 + row, s0 + c0, T::MINE, raw, good);

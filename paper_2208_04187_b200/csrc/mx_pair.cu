@@ -15,7 +15,8 @@
 //
 // What orders what: a stage's shared memory and scale columns are filled again once the commit of its products has come (to both
 // CTAs); products begin once both CTAs' codes have landed and both CTAs' scales are stored; a tile's accumulator is given back by all
-// 16 warps that read it.  Waits are bounded as in mx_matmul.cu; nobody leaves before the other's arrivals have come.
+// 16 warps that read it.  Waits are bounded as in mx_matmul.cu; nobody leaves before the other's arrivals have come.  Whoever gives up, neither CTA takes
+// a tile for summed whose last commit has not come to it.
 #include <cuda.h>          // types of tensor maps alone; the call comes from the runtime
 
 #include "mx_product.cuh"
@@ -173,7 +174,7 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
                 }
                 mxr_commit(&ctl->empty[slot]);
             }
-            mxr_commit(&ctl->done);
+            if (ok) mxr_commit(&ctl->done);
         }
         if (!ok) {                                                              // (what has been issued ends before the tensor memory goes)
             mxr_commit(&ctl->last);
@@ -214,18 +215,18 @@ mx_pair_kernel(const __grid_constant__ MxPairParams g) {
         const uint32_t row = (warp & 3u) * 32u + lane, c0 = (warp >> 2) * 128u;
         const uint32_t from = tmem + ((warp & 3u) << 21) + c0;
         uint32_t made = 0;
+        bool good = true;                   // (for good: behind a phase that never ended, the next one's parity reads as ended)
         for (uint32_t tile = first; tile < p.tiles; tile += step, ++made) {
             const uint32_t i = (tile % p.tiles_p * 2u + half) * 128u + row, j = tile / p.tiles_p * 256u + c0;
-            bool good = __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl, p.limit_ns));
+            good = good && __all_sync(0xFFFFFFFFu, mxp_wait(&ctl->done, made & 1u, ctl, p.limit_ns));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            good = good && !*(volatile uint32_t*)&ctl->failed;
             uint32_t raw[4][32];
             __syncwarp();
 #pragma unroll
             for (uint32_t c = 0; c < 4; ++c) mxp_load32(from + 32u * c, raw[c]);
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mxr_arrive_first(&ctl->taken);
+            if (lane == 0 && good) mxr_arrive_first(&ctl->taken);          // (the next tile waits for those who have read this one, and for them alone)
             mxp_row_any<128>(p, i, j, 128u, raw, good);
         }
     }

@@ -267,3 +267,31 @@ def test_a_product_whose_wait_cannot_end_returns(m, n, k, fmt, width, split, swa
         s = cta // split // -(-(n if swapped else m) // 128) * width
         assert part[:, s:s + width].isnan().all()
     assert torch.equal(lm.mx_matmul(qa, qb, torch.float32), want)
+
+
+@pytest.mark.parametrize("m, n, k, fmt, width, split, swapped, grid", STARVED)
+@pytest.mark.parametrize("cta, copy", [(0, 0), (1, 1), (5, 2), (6, 7)])
+def test_a_wait_that_cannot_end_gives_nan_for_its_part_alone(m, n, k, fmt, width, split, swapped, grid, cta, copy):
+    """Failure detection without a fault: a CTA waits for codes that nobody asks for, its 2 ms limit runs out, and whatever this CTA and its cluster have not
+    summed by then is NaN, in whole tiles; everything else is as ever."""
+    a, b = matrix(m, k, "bf16", 1, 0.5).cuda(), matrix(n, k, "bf16", 2, 0.5).cuda()
+    qa, qb = lm.mx_quantize(a, fmt), lm.mx_quantize(b, fmt)
+    want = lm.mx_matmul(qa, qb, torch.float32)
+    out = starved(qa, qb, m, n, k, fmt, cta, copy)
+    high, wide = (256, 256) if width == 512 else (128, width)
+    p, s = (n, m) if swapped else (m, n)
+    across = -(-p // high)
+    tiles, stages = across * -(-s // wide), -(-k // (128 if fmt == "e4m3" else 256))
+    unit, together = cta // split, grid // split
+    mine = range(unit, tiles, together)
+    if width < 256 and split > 1:                                  # a CTA of a cluster has a run of the stages
+        stages = stages * (cta % split + 1) // split - stages * (cta % split) // split
+    bad = torch.zeros(p, s, dtype=torch.bool, device="cuda")
+    if copy < len(mine) * stages:                                  # (else it asks for fewer, and nothing is left out)
+        for t in mine[copy // stages:]:
+            bad[t % across * high:(t % across + 1) * high, t // across * wide:(t // across + 1) * wide] = True
+        assert bad.any()
+    if swapped:
+        bad = bad.t()
+    assert torch.equal(out.isnan(), bad) and torch.equal(out[~bad], want[~bad])
+    assert torch.equal(lm.mx_matmul(qa, qb, torch.float32), want)     # the next call finds everything in order
