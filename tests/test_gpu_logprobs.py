@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import language_oracle as lo
-from paper_2208_04187_b200 import build
+from paper_2208_04187_b200 import binding, build
 from paper_2208_04187_b200 import language as lm
 
 pytestmark = pytest.mark.gpu
@@ -176,3 +176,20 @@ def test_rows_past_32_bits():
     got = lm.token_logprobs(x, t, top=1)
     assert abs(float(got.logprobs[rows - 1])) < 1e-6 and int(got.top_indices[rows - 1]) == vocab - 1
     assert abs(float(got.logprobs[rows - 2]) + np.log(vocab)) < 1e-4 and int(got.top_indices[rows - 2]) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_raw_pointers(dtype):
+    t = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    rows, vocab, top = 9, 1001, 4
+    x = torch.randn(rows, vocab, generator=torch.Generator().manual_seed(1)).to(t).cuda().requires_grad_()
+    targets = torch.arange(rows, device="cuda") * 100
+    got = lm.token_logprobs(x, targets, top=top)
+    dl, de = torch.linspace(-1, 1, rows, device="cuda"), torch.linspace(0.5, -0.5, rows, device="cuda")
+    (dx,) = torch.autograd.grad((got.logprobs, got.entropy), x, (dl, de))
+    lp, ent, stats, tops = (torch.empty(n, device="cuda") for n in (rows, rows, 2 * rows, rows * top))
+    idx, out, st, p = torch.empty(rows * top, dtype=torch.int64, device="cuda"), torch.empty_like(dx), binding.current_stream_handle(), torch.Tensor.data_ptr
+    binding.div_token_logprobs_forward(p(x), vocab, rows, vocab, dtype, p(targets), top, p(lp), p(ent), p(stats), p(tops), p(idx), st)
+    binding.div_token_logprobs_backward(p(x), vocab, rows, vocab, dtype, p(targets), p(stats), p(ent), p(dl), p(de), p(out), st)
+    assert torch.equal(lp, got.logprobs) and torch.equal(ent, got.entropy) and torch.equal(tops.view(rows, top), got.top_logprobs)
+    assert torch.equal(idx.view(rows, top), got.top_indices) and torch.equal(out, dx)

@@ -295,3 +295,48 @@ def test_a_wait_that_cannot_end_gives_nan_for_its_part_alone(m, n, k, fmt, width
         bad = bad.t()
     assert torch.equal(out.isnan(), bad) and torch.equal(out[~bad], want[~bad])
     assert torch.equal(lm.mx_matmul(qa, qb, torch.float32), want)     # the next call finds everything in order
+
+
+def check_on_the_device(y, a, b, dtype):
+    """As check_product, in 64 bits on the GPU."""
+    a, b = a.double(), b.double()
+    want, size = a @ b.t(), a.abs() @ b.abs().t()
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    bound = a.shape[1] * 2.0 ** -23 * size + half * want.abs() * (1 + 2.0 ** -10) + (2.0 ** -25 if dtype == "f16" else 0)
+    assert y.shape == want.shape and bool(((y.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("m, n, k, fmt", [(2300, 2200, 1100, "e4m3"), (2561, 4000, 3850, "e4m3"), (4097, 1025, 2050, "e4m3"), (2300, 2200, 1100, "e2m1"),
+                                          (777, 5000, 2720, "e2m1"), (2561, 4001, 3840, "e2m1")])
+def test_wide_tiles_past_the_first_turn_of_the_ring(m, n, k, fmt):
+    """Tiles of 256 columns whose stages go round the ring several times, more than one tile to a CTA; below the sizes that pairs take."""
+    dtype = ("f32", "bf16", "f16")[(m + n + k) % 3]
+    qa, qb = lm.mx_quantize(matrix(m, k, "bf16", m, 0.5).cuda(), fmt), lm.mx_quantize(matrix(n, k, "bf16", n + 1, 0.5).cuda(), fmt)
+    y = lm.mx_matmul(qa, qb, TYPES[dtype])
+    check_on_the_device(y, qa.dequantize(torch.float32), qb.dequantize(torch.float32), dtype)
+    assert torch.equal(lm.mx_matmul(qa, qb, TYPES[dtype]), y)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_large_linear_layer_and_its_gradients(fmt):
+    m, k, n = 2561, 3850, 4000
+    x, w, dy = matrix(m, k, "bf16", 1, 0.5).cuda().requires_grad_(), matrix(n, k, "bf16", 2, 0.5).cuda().requires_grad_(), matrix(m, n, "bf16", 3, 0.5).cuda()
+    y = lm.mx_linear(x, w, fmt=fmt)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+    q = lambda t: lm.mx_quantize(t.detach(), fmt).dequantize(torch.float32)  # noqa: E731
+    check_on_the_device(y, q(x), q(w), "bf16")
+    check_on_the_device(dx, q(dy), q(w.t()), "bf16")
+    check_on_the_device(dw, q(dy.t()), q(x.t()), "bf16")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_raw_pointers(fmt):
+    x = matrix(40, 300, "f16", 4).cuda()
+    rows, cols = lm.mx_quantize_both(x, fmt)
+    st = binding.current_stream_handle()
+    a, b = (torch.zeros(int(binding.div_mx_bytes(*s, fmt).total_bytes), dtype=torch.uint8, device="cuda") for s in ((40, 300), (300, 40)))
+    binding.div_mx_quantize(x.data_ptr(), 40, 300, 300, "f16", fmt, a.data_ptr(), a.numel(), b.data_ptr(), b.numel(), st)
+    for blob, q in ((a, rows), (b, cols)):
+        out = torch.empty(q.rows, q.cols, device="cuda")
+        binding.div_mx_dequantize(blob.data_ptr(), blob.numel(), q.rows, q.cols, fmt, out.data_ptr(), "f32", st)
+        assert torch.equal(out, q.dequantize(torch.float32))

@@ -164,3 +164,35 @@ def test_rows_behind_the_last_are_left_alone():
     binding.div_rms_norm_forward(x.data_ptr(), 104, None, 0, w.data_ptr(), "bf16", 3, 104, "bf16", 1e-6, None, out[1:].data_ptr(), None, 0, "e4m3", None,
                                  binding.current_stream_handle())
     assert (out[0] == 7).all() and (out[4] == 7).all() and torch.equal(out[1:4], lm.rms_norm(x, w)[0])
+
+
+# more rows than groups of threads, and no multiple of them: every size of group, aligned rows and others
+MANY = [(10007, 100, "bf16"), (10007, 104, "f32"), (3001, 520, "f16"), (3001, 521, "bf16"), (1000, 4096, "bf16"), (2500, 4096, "f32"), (1501, 2600, "bf16"),
+        (1501, 2601, "f16"), (701, 5000, "f16"), (701, 4999, "f32"), (500, 8192, "bf16"), (500, 8190, "bf16"), (900, 9001, "bf16"), (700, 16392, "f16")]
+
+
+@pytest.mark.parametrize("rows, cols, dtype", MANY)
+@pytest.mark.parametrize("fused", [False, True])
+def test_gradients_of_many_rows(rows, cols, dtype, fused):
+    """A group of threads goes from row to row: the next row's reads on their way, the weight's sums carried on, the long rows' in memory."""
+    groups = binding.div_rms_norm_workspace(rows, cols) // (4 * cols)
+    assert rows > groups and rows % groups
+    test_forward_and_gradients(rows, cols, dtype, fused)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_raw_pointers_backward(dtype):
+    rows, cols = 40, 264
+    dy, dh, x = (make(rows, cols, dtype, i).cuda() for i in range(3))
+    w = (1 + 0.3 * make(1, cols, "f32", 3)[0]).to(TYPES[dtype]).cuda()
+    a, r, v = x.clone().requires_grad_(), torch.zeros_like(x).requires_grad_(), w.clone().requires_grad_()
+    y, h = lm.rms_norm(a, v, r, eps=1e-5)
+    want = torch.autograd.grad((y, h), (a, v), (dy, dh))
+    st, p = binding.current_stream_handle(), torch.Tensor.data_ptr
+    out, hh, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda")
+    binding.div_rms_norm_forward(p(x), cols, p(r), cols, p(w), dtype, rows, cols, dtype, 1e-5, p(hh), p(out), None, 0, "e4m3", p(rstd), st)
+    assert torch.equal(out, y) and torch.equal(hh, h)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ws = torch.empty(binding.div_rms_norm_workspace(rows, cols), dtype=torch.uint8, device="cuda")
+    binding.div_rms_norm_backward(p(dy), cols, p(dh), cols, p(hh), cols, p(w), dtype, p(rstd), rows, cols, dtype, p(dx), p(dw), p(ws), ws.numel(), st)
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
