@@ -269,7 +269,7 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
             }
         }
     } else {
-        const uint32_t pieces = (p.cols + 7u) / 8u;
+        const uint32_t pieces = (p.cols + 7u) / 8u;                // (the group is the CTA, and every CTA has a first row: its sums are all written)
         for (uint32_t k = 0; k < rounds; ++k) {
             const uint64_t wide = (uint64_t)k * step + mine;
             const bool there = wide < p.rows;
@@ -304,9 +304,6 @@ norm_backward_kernel(const __grid_constant__ NormBackParams p) {
                 }
                 if (!pass) mean = norm_sum(dot, p.group, shared) * inv;
             }
-            if (!there && k == 0 && p.sums)                        // a group without rows
-                for (uint32_t at = t; at < pieces; at += p.group)
-                    for (uint32_t i = at * 8u; i < min(p.cols, at * 8u + 8u); ++i) sums[i] = 0.f;
         }
     }
 }
