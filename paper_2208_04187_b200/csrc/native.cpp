@@ -135,6 +135,18 @@ Tensor by_rows(const Tensor& t) {
     const bool runs = (t.size(1) <= 1 || t.stride(1) == 1) && (t.size(0) <= 1 || t.stride(0) >= t.size(1));
     return runs ? t : t.contiguous();
 }
+// leading dimensions folded into rows
+Tensor folded(const Tensor& t, const char* what) {
+    TORCH_CHECK_VALUE(t.dim() >= 1, what, " must be a tensor of at least one dimension");
+    TORCH_CHECK_VALUE(t.size(-1) != 0, what, " has rows of no numbers");
+    return t.dim() == 2 ? t : t.reshape({t.numel() / t.size(-1), t.size(-1)});
+}
+Tensor unfolded(const Tensor& t, const Tensor& like) {              // rows of `like`'s leading dimensions again
+    if (like.dim() == 2) return t;
+    auto sizes = like.sizes().vec();
+    sizes.back() = t.size(1);
+    return t.view(sizes);
+}
 void matrix(const Tensor& t, const char* what) {
     TORCH_CHECK_VALUE(t.is_cuda() && t.dim() == 2 && lm_type(t.scalar_type()) >= 0, what, " must be a CUDA matrix of float32, bfloat16 or float16");
 }
@@ -181,11 +193,12 @@ Tensor product(const Tensor& a, int64_t m, const Tensor& b, int64_t n, int64_t k
 }
 
 struct Normed {
-    Tensor y, blob, h, rstd;           // h: undefined without a residual
+    Tensor y, blob, h, rstd;           // y and h in x's shape; h: undefined without a residual
 };
-Normed norm(const Tensor& x0, const Tensor& r0, const Tensor& w0, double eps, bool want_y, int64_t format, bool want_rstd) {
+Normed norm(const Tensor& given, const Tensor& r_given, const Tensor& w0, double eps, bool want_y, int64_t format, bool want_rstd) {
+    const Tensor x0 = folded(given, "x"), r0 = r_given.defined() ? folded(r_given, "residual") : Tensor();
     matrix(x0, "x");
-    TORCH_CHECK_VALUE(!r0.defined() || (r0.device() == x0.device() && r0.scalar_type() == x0.scalar_type() && r0.sizes() == x0.sizes()),
+    TORCH_CHECK_VALUE(!r0.defined() || (r0.device() == x0.device() && r0.scalar_type() == x0.scalar_type() && r_given.sizes() == given.sizes()),
                       "residual must be like x: device, dtype and shape");
     TORCH_CHECK_VALUE(w0.device() == x0.device() && w0.dim() == 1 && w0.size(0) == x0.size(1) && (w0.scalar_type() == x0.scalar_type() || w0.scalar_type() == at::kFloat),
                       "weight must have one number a column, x's dtype or float32, on x's device");
@@ -193,9 +206,9 @@ Normed norm(const Tensor& x0, const Tensor& r0, const Tensor& w0, double eps, bo
     const Tensor x = by_rows(x0), r = r0.defined() ? by_rows(r0) : Tensor(), w = w0.contiguous();
     const int64_t rows = x.size(0), cols = x.size(1);
     Normed n;
-    if (want_y) n.y = fresh({rows, cols}, x.scalar_type(), x);
+    if (want_y) n.y = fresh(given.sizes(), x.scalar_type(), x);
     if (format >= 0) n.blob = new_blob(x, rows, cols, format);
-    if (r.defined()) n.h = fresh({rows, cols}, x.scalar_type(), x);
+    if (r.defined()) n.h = fresh(given.sizes(), x.scalar_type(), x);
     if (want_rstd) n.rstd = fresh({rows}, at::kFloat, x);
     check(div_rms_norm_forward(x.data_ptr(), x.stride(0), at_(r), r.defined() ? r.stride(0) : 0, w.data_ptr(), lm_type(w.scalar_type()), rows, cols,
                                lm_type(x.scalar_type()), (float)eps, at_(n.h), at_(n.y), at_(n.blob), bytes_of(n.blob), (int32_t)format, (float*)at_(n.rstd),
@@ -205,7 +218,8 @@ Normed norm(const Tensor& x0, const Tensor& r0, const Tensor& w0, double eps, bo
 struct NormGrads {
     Tensor dx, dw;
 };
-NormGrads norm_backward(const Tensor& dy0, const Tensor& dh0, const Tensor& h0, const Tensor& w0, const Tensor& rstd, bool want_dw) {
+NormGrads norm_backward(const Tensor& dy_given, const Tensor& dh_given, const Tensor& h_given, const Tensor& w0, const Tensor& rstd, bool want_dw) {
+    const Tensor dy0 = folded(dy_given, "dy"), dh0 = dh_given.defined() ? folded(dh_given, "dh") : Tensor(), h0 = folded(h_given, "h");
     for (const Tensor* t : {&dy0, &dh0})
         TORCH_CHECK_VALUE(!t->defined() || (t->device() == h0.device() && t->scalar_type() == h0.scalar_type() && t->sizes() == h0.sizes()),
                           "gradients must be like h: device, dtype and shape");
@@ -213,7 +227,7 @@ NormGrads norm_backward(const Tensor& dy0, const Tensor& dh0, const Tensor& h0, 
     const Tensor dy = by_rows(dy0), dh = dh0.defined() ? by_rows(dh0) : Tensor(), h = by_rows(h0), w = w0.contiguous();
     const int64_t rows = h.size(0), cols = h.size(1);
     NormGrads g;
-    g.dx = fresh({rows, cols}, h.scalar_type(), h);
+    g.dx = fresh(h_given.sizes(), h.scalar_type(), h);
     Tensor ws;
     if (want_dw) {
         uint64_t bytes = 0;
@@ -289,6 +303,7 @@ struct LinearFn : Function<LinearFn> {                       // y = Q(x) Q(w)^T,
     }
 };
 
+// (x and h are kept in the shape that they were given in: what saved-tensor hooks do to a map they do by its shape)
 struct NormFn : Function<NormFn> {
     static variable_list forward(AutogradContext* ctx, const Tensor& x, const std::optional<Tensor>& given, const Tensor& w, double eps) {
         const Tensor r = given ? *given : Tensor();
@@ -321,7 +336,7 @@ struct NormLinearFn : Function<NormLinearFn> {
         ctx->saved_data["eps"] = eps;
         ctx->saved_data["type"] = (int64_t)w.scalar_type();
         ctx->saved_data["outs"] = w.size(0);
-        Tensor out = product(n.blob, x.size(0), qw.rows, w.size(0), x.size(1), format, x.scalar_type());
+        Tensor out = product(n.blob, x.numel() / x.size(-1), qw.rows, w.size(0), x.size(-1), format, x.scalar_type());
         if (!r.defined()) return {out};
         return {out, n.h};
     }
@@ -331,14 +346,14 @@ struct NormLinearFn : Function<NormLinearFn> {
         if (!g[0].defined()) return {dh, fused ? dh : Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
         const variable_list kept = ctx->get_saved_variables();
         const Tensor &h = kept[0], &weight = kept[1], &rstd = kept[2];
-        const int64_t format = ctx->saved_data["format"].toInt(), n = ctx->saved_data["outs"].toInt(), m = h.size(0), k = h.size(1);
+        const int64_t format = ctx->saved_data["format"].toInt(), n = ctx->saved_data["outs"].toInt(), k = h.size(-1), m = h.numel() / k;
         const int at = 1 + fused;                             // of the norm's weight among the inputs that are there
         const bool need_w = ctx->needs_input_grad(at + 1);
         const Quantised q = quantise(g[0], format, true, need_w);
         Tensor dw;
         if (need_w) {
             const Normed y = norm(h, Tensor(), weight, ctx->saved_data["eps"].toDouble(), true, -1, false);
-            dw = product(q.cols, n, quantise(y.y, format, false, true).cols, k, m, format, (at::ScalarType)ctx->saved_data["type"].toInt());
+            dw = product(q.cols, n, quantise(folded(y.y, "y"), format, false, true).cols, k, m, format, (at::ScalarType)ctx->saved_data["type"].toInt());
         }
         const Tensor dy = product(q.rows, m, kept[3], k, n, format, h.scalar_type());
         const NormGrads d = norm_backward(dy, dh, h, weight, rstd, ctx->needs_input_grad(at));
@@ -423,18 +438,6 @@ bool format_arg(PyObject* o, int64_t* out) {
 bool count_is(Py_ssize_t n, Py_ssize_t want) {
     if (n != want) PyErr_Format(PyExc_TypeError, "takes %zd arguments", want);
     return n == want;
-}
-// leading dimensions folded into rows
-Tensor folded(const Tensor& t, const char* what) {
-    TORCH_CHECK_VALUE(t.dim() >= 1, what, " must be a tensor of at least one dimension");
-    TORCH_CHECK_VALUE(t.size(-1) != 0, what, " has rows of no numbers");
-    return t.dim() == 2 ? t : t.reshape({t.numel() / t.size(-1), t.size(-1)});
-}
-Tensor unfolded(const Tensor& t, const Tensor& like) {              // rows of `like`'s leading dimensions again
-    if (like.dim() == 2) return t;
-    auto sizes = like.sizes().vec();
-    sizes.back() = t.size(1);
-    return t.view(sizes);
 }
 PyObject* wrapped(std::initializer_list<Tensor> all) {             // a tuple; None for what is not there
     PyObject* out = PyTuple_New((Py_ssize_t)all.size());
@@ -561,23 +564,21 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-bool norm_args(PyObject* x, PyObject* r, PyObject* w, PyObject* e, Tensor* given, Tensor* flat, Tensor* res, Tensor* weight, double* eps) {
+bool norm_args(PyObject* x, PyObject* r, PyObject* w, PyObject* e, Tensor* given, Tensor* res, Tensor* weight, double* eps) {
     if (!given_tensor(x, given) || !maybe_tensor(r, res) || !given_tensor(w, weight) || !real(e, eps)) return false;
-    *flat = folded(*given, "x");
-    if (res->defined()) {
-        TORCH_CHECK_VALUE(res->sizes() == given->sizes(), "residual must have the shape of x");
-        *res = folded(*res, "residual");
-    }
+    TORCH_CHECK_VALUE(given->dim() >= 1, "x must be a tensor of at least one dimension");
+    TORCH_CHECK_VALUE(given->size(-1) != 0, "x has rows of no numbers");
+    TORCH_CHECK_VALUE(!res->defined() || res->sizes() == given->sizes(), "residual must have the shape of x");
     return true;
 }
 
 // rms_norm(x, residual or None, weight, eps) -> (y, h); h is x without a residual
 PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Tensor given, x, r, w, y, h;
+    Tensor x, r, w, y, h;
     double eps;
-    if (!count_is(n, 4) || !norm_args(a[0], a[1], a[2], a[3], &given, &x, &r, &w, &eps)) return nullptr;
-    if (x.size(0) == 0) return wrapped({no_rows(given, x.size(1), {&x, &r, &w}), r.defined() ? given + unfolded(r, given) : given});
+    if (!count_is(n, 4) || !norm_args(a[0], a[1], a[2], a[3], &x, &r, &w, &eps)) return nullptr;
+    if (x.numel() == 0) return wrapped({no_rows(x, x.size(-1), {&x, &r, &w}), r.defined() ? x + r : x});
     if (!ran("div_rms_norm", [&] {
             if (wants_grad({&x, &r, &w})) {
                 const variable_list got = NormFn::apply(x, r.defined() ? std::optional<Tensor>(r) : std::nullopt, w, eps);
@@ -590,38 +591,38 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
             }
         }))
         return nullptr;
-    return wrapped({unfolded(y, given), h.defined() ? unfolded(h, given) : given});
+    return wrapped({y, h.defined() ? h : x});
     END_HANDLE_TH_ERRORS
 }
 
 // rms_norm_mx(x, residual or None, weight, eps, format) -> (blob, rows, columns, h)
 PyObject* rms_norm_mx(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Tensor given, x, r, w;
+    Tensor x, r, w;
     double eps;
     int64_t format;
-    if (!count_is(n, 5) || !format_arg(a[4], &format) || !norm_args(a[0], a[1], a[2], a[3], &given, &x, &r, &w, &eps)) return nullptr;
+    if (!count_is(n, 5) || !format_arg(a[4], &format) || !norm_args(a[0], a[1], a[2], a[3], &x, &r, &w, &eps)) return nullptr;
     Normed got;
-    if (x.size(0) == 0) {
+    if (x.numel() == 0) {
         got.blob = at::empty({0}, x.options().dtype(at::kByte));
         if (r.defined()) got.h = x + r;
     } else if (!ran("div_rms_norm_forward", [&] { got = norm(x, r, w, eps, false, format, false); })) {
         return nullptr;
     }
-    PyObject *blob = THPVariable_Wrap(got.blob), *h = THPVariable_Wrap(got.h.defined() ? unfolded(got.h, given) : given);
-    return Py_BuildValue("NLLN", blob, (long long)x.size(0), (long long)x.size(1), h);
+    PyObject *blob = THPVariable_Wrap(got.blob), *h = THPVariable_Wrap(got.h.defined() ? got.h : x);
+    return Py_BuildValue("NLLN", blob, (long long)(x.numel() / x.size(-1)), (long long)x.size(-1), h);
     END_HANDLE_TH_ERRORS
 }
 
 // mx_norm_linear(x, residual or None, norm weight, w, eps, format) -> (out, h)
 PyObject* mx_norm_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Tensor given, x, r, g, w, out, h;
+    Tensor x, r, g, w, out, h;
     double eps;
     int64_t format;
-    if (!count_is(n, 6) || !format_arg(a[5], &format) || !given_tensor(a[3], &w) || !norm_args(a[0], a[1], a[2], a[4], &given, &x, &r, &g, &eps)) return nullptr;
+    if (!count_is(n, 6) || !format_arg(a[5], &format) || !given_tensor(a[3], &w) || !norm_args(a[0], a[1], a[2], a[4], &x, &r, &g, &eps)) return nullptr;
     weight_fits(x, w);
-    if (x.size(0) == 0) return wrapped({no_rows(given, w.size(0), {&x, &r, &g, &w}), r.defined() ? given + unfolded(r, given) : given});
+    if (x.numel() == 0) return wrapped({no_rows(x, w.size(0), {&x, &r, &g, &w}), r.defined() ? x + r : x});
     if (!ran("mx_norm_linear", [&] {
             if (wants_grad({&x, &r, &g, &w})) {
                 const variable_list got = NormLinearFn::apply(x, r.defined() ? std::optional<Tensor>(r) : std::nullopt, g, w, eps, format);
@@ -630,11 +631,11 @@ PyObject* mx_norm_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
             } else {
                 const Normed got = norm(x, r, g, eps, false, format, false);
                 h = got.h;
-                out = product(got.blob, x.size(0), quantise(w, format, true, false).rows, w.size(0), x.size(1), format, x.scalar_type());
+                out = product(got.blob, x.numel() / x.size(-1), quantise(w, format, true, false).rows, w.size(0), x.size(-1), format, x.scalar_type());
             }
         }))
         return nullptr;
-    return wrapped({unfolded(out, given), h.defined() ? unfolded(h, given) : given});
+    return wrapped({unfolded(out, x), h.defined() ? h : x});
     END_HANDLE_TH_ERRORS
 }
 

@@ -7,6 +7,7 @@ import torch
 from oracle import language_oracle as lo
 from paper_2208_04187_b200 import build
 from paper_2208_04187_b200 import language as lm
+from paper_2208_04187_b200.autograd import DivisionCache
 
 pytestmark = pytest.mark.gpu
 
@@ -268,3 +269,59 @@ def test_a_replaced_norm_gives_what_torchs_gave(dtype):
     # both: a sum of 64 and a handful of operations in 32 bits, then half a step
     size = want.double().abs()
     assert ((got.double() - want.double()).abs() <= 2 * (torch.finfo(dtype).eps / 2 + 40 * 2.0 ** -24) * (1 + 2.0 ** -8) * size).all()
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_a_norm_under_the_activation_cache(fused):
+    """What a norm keeps of a map of 3 dimensions is a map of 3 dimensions: the cache takes it, and the gradients are the formula's at the map that
+    comes back."""
+    b, t, d = 4, 64, 256
+    x, w = make(b, t, d, seed=1, dtype=torch.float32).cuda().requires_grad_(), (1 + make(d, seed=2, scale=0.1, dtype=torch.float32)).cuda().requires_grad_()
+    r = make(b, t, d, seed=3, dtype=torch.float32).cuda().requires_grad_() if fused else None
+    dy = make(b, t, d, seed=4, dtype=torch.float32).cuda()
+    back = []
+
+    class Watched(DivisionCache):
+        def unpack(self, h):
+            back.append(super().unpack(h))
+            return back[-1]
+    with Watched(block=8, qbits=8) as cache:
+        y, h = lm.rms_norm(x * 1, w, r, eps=1e-5)
+    assert cache.maps == 1 and y.shape == h.shape == (b, t, d)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+    (kept,) = [u for u in back if u.shape == (b, t, d)]
+    assert not torch.equal(kept, h) and kept.isfinite().all()
+    n64 = f64(h).reshape(-1, d)
+    rstd = 1 / np.sqrt((n64 * n64).mean(1) + 1e-5)
+    want, want_w = lo.rms_norm_backward(f64(dy).reshape(-1, d), None, f64(kept).reshape(-1, d), f64(w), rstd)
+    # every term of a sum to 300 steps in 32 bits (no sum here has more)
+    size = rstd[:, None] * np.abs(f64(dy).reshape(-1, d) * f64(w))
+    n = np.abs(f64(kept).reshape(-1, d)) * rstd[:, None]
+    bound = size + n * (size * n).mean(1, keepdims=True)
+    assert (np.abs(f64(dx).reshape(-1, d) - want) <= 300 * 2.0 ** -24 * bound).all()
+    assert (np.abs(f64(dw) - want_w) <= 300 * 2.0 ** -24 * (np.abs(f64(dy).reshape(-1, d)) * n).sum(0)).all()
+
+
+def test_shapes_of_norms_and_layers():
+    """Outputs and gradients have the shapes of what was given, rows apart or folded."""
+    d = 96
+    g, w = torch.ones(d, device="cuda", dtype=torch.bfloat16).requires_grad_(), make(40, d, seed=1).cuda().requires_grad_()
+    for shape in ((d,), (5, d), (2, 3, d), (2, 1, 3, d)):
+        x, r = make(*shape, seed=2).cuda().requires_grad_(), make(*shape, seed=3).cuda().requires_grad_()
+        for residual in (None, r):
+            y, h = lm.rms_norm(x, g, residual)
+            out, k = lm.mx_norm_linear(x, g, w, residual)
+            q, z = lm.rms_norm_mx(x, g, residual)
+            assert y.shape == h.shape == k.shape == z.shape == shape and out.shape == shape[:-1] + (40,) and torch.equal(h, k) and torch.equal(h, z)
+            assert q.shape == (x.numel() // d, d) and torch.equal(lm.mx_matmul(q, lm.mx_quantize(w)), out.view(-1, 40))
+            flat, _ = lm.rms_norm(x.detach().reshape(-1, d), g, None if residual is None else residual.detach().reshape(-1, d))
+            assert torch.equal(y.view(-1, d), flat)
+            leaves = [x, g] + ([r] if residual is not None else [])
+            for o in (y, out):
+                for leaf, grad in zip(leaves, torch.autograd.grad((o.float() * torch.arange(o.size(-1), device="cuda")).sum(), leaves)):
+                    assert grad.shape == leaf.shape and grad.isfinite().all() and grad.abs().sum() > 0
+            h.mul_(1) if residual is not None else None              # (no view that torch would forbid to change)
+    a, b = make(6, 5, d, seed=4).cuda().transpose(0, 1), make(6, 5, 2 * d, seed=5).cuda()[..., :d].transpose(0, 1)
+    y, h = lm.rms_norm(a, g, b)
+    z, k = lm.rms_norm(a.contiguous(), g, b.contiguous())
+    assert torch.equal(y, z) and torch.equal(h, k)
