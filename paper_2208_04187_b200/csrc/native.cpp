@@ -324,12 +324,12 @@ struct NormFn : Function<NormFn> {
     }
 };
 
-// The norm's output goes into the product in few bits and is not kept: backward makes it again from h and rstd.
+// The norm's output goes into the product in few bits and is not kept: backward makes it again from h.
 struct NormLinearFn : Function<NormLinearFn> {
     static variable_list forward(AutogradContext* ctx, const Tensor& x, const std::optional<Tensor>& given, const Tensor& g, const Tensor& w, double eps, int64_t format) {
         const Tensor r = given ? *given : Tensor();
         Normed n = norm(x, r, g, eps, false, format, true);
-        const Quantised qw = quantise(w, format, true, true);
+        const Quantised qw = quantise(w, format, true, x.requires_grad() || (r.defined() && r.requires_grad()) || g.requires_grad());
         ctx->save_for_backward({r.defined() ? n.h : x, g, n.rstd, qw.cols});
         ctx->set_materialize_grads(false);
         ctx->saved_data["format"] = format;
@@ -349,14 +349,18 @@ struct NormLinearFn : Function<NormLinearFn> {
         const int64_t format = ctx->saved_data["format"].toInt(), n = ctx->saved_data["outs"].toInt(), k = h.size(-1), m = h.numel() / k;
         const int at = 1 + fused;                             // of the norm's weight among the inputs that are there
         const bool need_w = ctx->needs_input_grad(at + 1);
-        const Quantised q = quantise(g[0], format, true, need_w);
+        const bool need_h = kept[3].defined() && (ctx->needs_input_grad(0) || (fused && ctx->needs_input_grad(1)) || ctx->needs_input_grad(at));
         Tensor dw;
-        if (need_w) {
-            const Normed y = norm(h, Tensor(), weight, ctx->saved_data["eps"].toDouble(), true, -1, false);
-            dw = product(q.cols, n, quantise(folded(y.y, "y"), format, false, true).cols, k, m, format, (at::ScalarType)ctx->saved_data["type"].toInt());
+        NormGrads d;
+        if (need_h || need_w) {
+            const Quantised q = quantise(g[0], format, need_h, need_w);
+            if (need_w) {
+                // (y in h's type, as rms_norm gives it: one rounding ahead of that to 8 or 4 bits, for half the bytes of 32-bit values)
+                const Normed y = norm(h, Tensor(), weight, ctx->saved_data["eps"].toDouble(), true, -1, false);
+                dw = product(q.cols, n, quantise(folded(y.y, "y"), format, false, true).cols, k, m, format, (at::ScalarType)ctx->saved_data["type"].toInt());
+            }
+            if (need_h) d = norm_backward(product(q.rows, m, kept[3], k, n, format, h.scalar_type()), dh, h, weight, rstd, ctx->needs_input_grad(at));
         }
-        const Tensor dy = product(q.rows, m, kept[3], k, n, format, h.scalar_type());
-        const NormGrads d = norm_backward(dy, dh, h, weight, rstd, ctx->needs_input_grad(at));
         variable_list out = once({d.dx, d.dw, dw});
         return {out[0], fused ? out[0] : Tensor(), out[1], out[2], Tensor(), Tensor()};
     }

@@ -112,8 +112,9 @@ def rms_norm_mx(x, weight, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
 
 
 def mx_norm_linear(x, norm_weight, w, residual=None, eps: float = 1e-6, fmt: str = "e4m3"):
-    """(out, h): the norm and the linear layer behind it.  The norm's output goes into the product in few bits and is not kept: the
-    backward pass makes it again from h and one number a row.  Gradients as of mx_linear and rms_norm."""
+    """(out, h): the norm and the linear layer behind it.  The norm's output goes into the product in few bits, quantised from its 32-bit
+    values, and is not kept: the backward pass makes it again from h, rounded to x's dtype, for the gradient of w.  Gradients as of
+    rms_norm and, at its result, of mx_linear."""
     return (_native or _load()).mx_norm_linear(x, residual, norm_weight, w, eps, fmt)
 
 

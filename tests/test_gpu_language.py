@@ -325,3 +325,34 @@ def test_shapes_of_norms_and_layers():
     y, h = lm.rms_norm(a, g, b)
     z, k = lm.rms_norm(a.contiguous(), g, b.contiguous())
     assert torch.equal(y, z) and torch.equal(h, k)
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_a_frozen_norm_costs_its_layer_nothing(fused):
+    """Where the weight alone wants a gradient, neither the weight's columns are kept nor a gradient of the norm made."""
+    m, d, n = 512, 1024, 2048
+    x, g, w = make(m, d, seed=1).cuda(), (1 + make(d, seed=2, scale=0.1)).cuda(), make(n, d, seed=3).cuda()
+    r, dy = make(m, d, seed=4).cuda() if fused else None, make(m, n, seed=5).cuda()
+
+    def kept(*leaves):
+        for t in leaves:
+            t.requires_grad_()
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        out, h = lm.mx_norm_linear(x, g, w, r, fmt="e4m3")
+        size = torch.cuda.memory_allocated() - before - 2 * out.numel() - (2 * h.numel() if fused else 0)
+        grads = torch.autograd.grad(out, leaves, dy)
+        for t in leaves:
+            t.requires_grad_(False)
+        return size, grads
+    alone, (dw,) = kept(w)
+    both, (dw2, dg) = kept(w, g)
+    assert torch.equal(dw, dw2) and dg.abs().sum() > 0
+    blob = n * d * 33 // 32
+    assert alone <= 16 * 1024 and both >= blob                    # alone: a number a row
+    # a leaf that this call does not ask for
+    w.requires_grad_(), x.requires_grad_()
+    out, _ = lm.mx_norm_linear(x, g, w, r, fmt="e4m3")
+    assert torch.equal(torch.autograd.grad(out, w, dy, retain_graph=True)[0], dw)
+    dx = torch.autograd.grad(out, x, dy)[0]
+    assert dx.shape == x.shape and dx.abs().sum() > 0
