@@ -641,13 +641,15 @@ div_status div_token_logprobs_forward(const void* logits_dev, int64_t row_stride
         cfg.blockDim = dim3(LP_THREADS);
         cfg.stream = (cudaStream_t)cuda_stream;
         // Fewer CTAs than places: some SMs would get 6 while others get 2.  Shared memory that nobody uses leaves as many places as an even
-        // share takes (500 rows of 100003 bf16 37 -> 29 us, 250 of 131072 in clusters of two 25.6 -> 20.3, 500 of 2000 5.7 -> 4.7; 300 of 131072
-        // 24.9 -> 27.3).  Larger clusters need the room to be placed.
+        // share takes.  For 16-bit types and shares of 4 and 5 only: 131072 bf16 with 5 alternatives, 260 rows in clusters of two 27.7 -> 22.2 us,
+        // 450 rows 45.4 -> 35.5, 600 46.7 -> 42.9, 740 42.2 -> 45.7; of 32000 260 14.4 -> 11.6, 592 12.4 -> 12.8.  With shares of 2 and 3 it gives
+        // nothing (300 rows 27.2 and 28.0, 400 29.2 and 29.4), and float32 takes longer with any (50257 numbers, 300 rows 18.3 and 22.4, 500 26.1
+        // and 30.8, 650 28.9 and 40.0).
         const uint32_t share = ((uint32_t)rows * split + 147u) / 148u;
-        if (split <= 2u && share < LP_RESIDENT && share > 1u) {
+        if (sizeof(XT) == 2 && split <= 2u && share < LP_RESIDENT && share > 3u) {
             static SmemAllowed allowed[2];
             cfg.dynamicSmemBytes = LP_SMEM / share - 5u * 1024u;              // (what a CTA has besides: its own 3.7 KB, the system's 1 KB)
-            if (!allowed[top ? 1 : 0]((const void*)kern, LP_SMEM / 2u)) return DIV_ERR_CUDA;
+            if (!allowed[top ? 1 : 0]((const void*)kern, LP_SMEM / 4u)) return DIV_ERR_CUDA;
         }
         cudaLaunchAttribute at[2];
         at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
