@@ -482,10 +482,10 @@ div_status product(MxProductParams p, bool starved, const void* a_dev, size_t a_
     if (bn == 128u && blocks_p * ((rows_s + 255u) / 256u) >= 120u) bn = 256u;
     const auto tiles_of = [&](uint32_t width) { return blocks_p * ((rows_s + width - 1u) / width); };
     if (tiles_of(bn) >= (1ull << 31)) return DIV_ERR_SHAPE;
-    // large products of e2m1: by pairs of CTAs, whose start and end take longer than they save with rows of less than 4096 numbers or fewer
-    // than two rounds of tiles (mx_pair.cu has both sides' times; it counts rows of 128 bytes in 31 bits)
+    // large products of e2m1: by pairs of CTAs, whose start and end take longer than they save with short rows or fewer than two rounds of tiles
+    // (mx_pair.cu has both sides' times; it counts rows of 128 bytes in 31 bits)
     const uint64_t paired = (blocks_p + 1u) / 2u * ((rows_s + 255u) / 256u);
-    if (format == MX_E2M1 && bn == 256u && p.p.s.stages >= 16u && paired >= MXP_SMS && ((mx_codes_bytes(p.p.s) | mx_codes_bytes(p.s.s)) >> 38) == 0) {
+    if (format == MX_E2M1 && bn == 256u && p.p.s.stages >= 11u && paired >= MXP_SMS && ((mx_codes_bytes(p.p.s) | mx_codes_bytes(p.s.s)) >> 38) == 0) {
         p.tiles_p = (uint32_t)((blocks_p + 1u) / 2u);
         p.tiles = (uint32_t)paired;
         p.split = 1;

@@ -9,9 +9,13 @@
 // stage of e2m1.  Here four warps read them from shared memory and store them to their quarter of the lanes, while earlier stages are
 // multiplied; all 8 warps of a pair report to the first CTA before it issues the stage.
 //
-// 8192 x 8192 x 8192 242 us (CTAs alone 280), 8192 x 8192 x 4096 145 us (171), 4096 x 4096 x 4096 46 us (46), of fewer than
-// 4096 a row longer than alone: 5000 x 3000 x 2000 31 us (29).  For e4m3, with 3 copies of scales a stage, the two are equal (8192 x 8192
-// x 8192 474 and 477 us).
+// Pairs and CTAs alone, us, back to back, rows of k numbers (k at the end):
+//   8192 x 8192 x  2048 96.2 and 89.8   2560 98.1 and 100.8   2816 99.0 and 106.5   3584 114 and 125   4096 126 and 138
+//   4096 x 4096 x  2048 28.3 and 27.0   2816 31.4 and 31.5    3584 35.8 and 37.6    4096 38.6 and 41.1   8192 62.3 and 69.9
+//   16384 x 8192 x 2048 184 and 170     2816 195 and 194      3584 225 and 230;     5000 x 5000 x 2048 39.5 and 39.4   2816 44.4 and 48.0
+//   2304 x 4096 x 4096 (144 tiles, one round and a little more) 23.7 and 23.3, 3000 x 3100 x 4096 (156) 28.9 and 29.4
+// so that pairs begin at 11 stages (2561 numbers) and 148 tiles.  For e4m3, with 3 copies of scales a stage, the two are equal (8192 x 8192 x 8192
+// 474 and 477 us).
 //
 // What orders what: a stage's shared memory and scale columns are filled again once the commit of its products has come (to both
 // CTAs); products begin once both CTAs' codes have landed and both CTAs' scales are stored; a tile's accumulator is given back by all

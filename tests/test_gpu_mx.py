@@ -340,3 +340,14 @@ def test_raw_pointers(fmt):
         out = torch.empty(q.rows, q.cols, device="cuda")
         binding.div_mx_dequantize(blob.data_ptr(), blob.numel(), q.rows, q.cols, fmt, out.data_ptr(), "f32", st)
         assert torch.equal(out, q.dequantize(torch.float32))
+
+
+@pytest.mark.parametrize("k", [2560, 2561, 3000, 3841])
+def test_four_bit_products_on_both_sides_of_the_pairs_border(k):
+    """Sums of whole numbers below 2^24: exact, whichever kernel takes them."""
+    g = torch.Generator("cuda").manual_seed(k)
+    a, b = (torch.randint(-6, 7, (r, k), generator=g, device="cuda").float() for r in (3500, 3300))
+    a[:, ::32], b[:, ::32] = 6, 6
+    qa, qb = lm.mx_quantize(a, "e2m1"), lm.mx_quantize(b, "e2m1")
+    want = qa.dequantize(torch.float32).double() @ qb.dequantize(torch.float32).double().t()
+    assert torch.equal(lm.mx_matmul(qa, qb, torch.float32).double(), want)
