@@ -286,14 +286,20 @@ mx_product_kernel(const __grid_constant__ MxProductParams p) {
 // column would be used, and its way out through a cluster takes as long as everything else.  Here a CTA takes 8 rows of P; its 4 warps
 // share the stages, 8 lanes a row's stage, a block of 32 numbers each.  S lies in shared memory in 16 bits.  A block sums exactly in
 // 16 bits (8 products of at most 36, in steps of 1/4, to a half of a register); the block's sum is scaled by both powers of two at once.
-// From L2, against the tensor cores' kernel: 1024 x 1024 1.9 us (4.3), 4096 x 4096 5.1 us (6.1); 8192 x 8192 12.2 us (10.4), which turning
-// codes into numbers takes.  (The same for e4m3, whose products need 32 bits, took 7.6 us at 4096 x 4096, the tensor cores 6.8; for two
-// tokens 6.4 us, the tensor cores 6.1.)
+// (The same for e4m3, whose products need 32 bits, took 7.6 us at 4096 x 4096, the tensor cores 6.8; for two tokens 6.4 us, the tensor cores 6.1.)
+// From L2, us, against the tensor cores' kernel (rows x numbers a row):
+//    512 x  8192  4.8 and  5.3     1024 x 2048 2.3 and 4.2    4096 x 2048 3.5 and 4.9     8192 x  512 3.8 and 3.1
+//    512 x 12000  6.5 and  6.1     1024 x 4096 3.0 and 4.7    4096 x 4096 5.2 and 5.7     8192 x 2048 5.1 and 5.1
+//   1024 x 16384  8.4 and  7.0     1024 x 8192 4.8 and 5.5    4096 x 6000 7.4 and 6.5    10000 x 1024 4.5 and 7.6
+//   2048 x  8192  5.5 and 10.2     3000 x 4096 5.0 and 5.4    6000 x 2048 4.5 and 4.9    12288 x  512 5.0 and 3.3
+//   3000 x  6000  7.1 and  6.2     3000 x 8192 8.5 and 6.9    6000 x 4096 6.6 and 6.4    16384 x 1024 6.0 and 4.2
+// It takes longer with more than 32 stages (each warp goes through a quarter of them, one after another), with rows of more than a CTA's worth
+// for all places of the device (each CTA turns the token into numbers again), and past 65536 rows x stages.
 constexpr uint32_t MXV_THREADS = 128, MXV_ROWS = 8;
-constexpr uint64_t MXV_MOST = 4096u * 16u;                 // rows x stages up to which this kernel is the shorter
-constexpr uint32_t MXV_MAX_SMEM = 96u * 1024u;             // of S: values and scale bytes
+constexpr uint32_t MXV_MOST = 65536u, MXV_MAX_ROWS = 10240u, MXV_MAX_STAGES = 32u;      // rows x stages, and each, up to which this kernel is the shorter
 
-__host__ __device__ inline uint32_t mxv_smem(uint32_t stages) { return stages * (512u + 8u); }
+__host__ __device__ constexpr uint32_t mxv_smem(uint32_t stages) { return stages * (512u + 8u); }       // of S: values and scale bytes
+static_assert(mxv_smem(MXV_MAX_STAGES) + 4u * MXV_ROWS * 4u <= 48u * 1024u, "no leave to ask for");
 // dot * 2^(a - 127) * 2^(b - 127)
 __device__ __forceinline__ float mxv_scaled(float dot, uint32_t a, uint32_t b) {
     if (a == 255u || b == 255u) return __uint_as_float(0x7FC00000u);
@@ -407,8 +413,6 @@ namespace {
 using namespace divk;
 
 div_status vector_launch(const MxProductParams& p, cudaStream_t st) {
-    static SmemAllowed allowed;
-    if (!allowed((const void*)mx_vector_kernel, MXV_MAX_SMEM)) return DIV_ERR_CUDA;
     return launch_pdl(mx_vector_kernel, dim3((p.p.s.rows + MXV_ROWS - 1u) / MXV_ROWS), MXV_THREADS, mxv_smem(p.p.s.stages), st, p);
 }
 
@@ -474,7 +478,7 @@ div_status product(MxProductParams p, bool starved, const void* a_dev, size_t a_
     p.out = out_dev;
     p.ld = (uint64_t)out_row_stride;
     p.out_dtype = (uint32_t)out_dtype;
-    if (format == MX_E2M1 && p.s.s.rows == 1u && (uint64_t)p.p.s.rows * p.p.s.stages <= MXV_MOST && p.p.s.stages <= MXV_MAX_SMEM / mxv_smem(1u))
+    if (format == MX_E2M1 && p.s.s.rows == 1u && p.p.s.rows <= MXV_MAX_ROWS && p.p.s.stages <= MXV_MAX_STAGES && p.p.s.rows * p.p.s.stages <= MXV_MOST)
         return starved ? DIV_ERR_PARAM : vector_launch(p, (cudaStream_t)cuda_stream);
     const uint64_t rows_s = p.s.s.rows;
     const uint64_t blocks_p = (p.p.s.rows + 127u) / 128u;

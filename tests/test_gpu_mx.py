@@ -351,3 +351,15 @@ def test_four_bit_products_on_both_sides_of_the_pairs_border(k):
     qa, qb = lm.mx_quantize(a, "e2m1"), lm.mx_quantize(b, "e2m1")
     want = qa.dequantize(torch.float32).double() @ qb.dequantize(torch.float32).double().t()
     assert torch.equal(lm.mx_matmul(qa, qb, torch.float32).double(), want)
+
+
+@pytest.mark.parametrize("n, k", [(512, 8192), (512, 8193), (10240, 1024), (10241, 1024), (4096, 4096), (4097, 4096), (65, 16400)])
+def test_one_token_of_4_bits_on_both_sides_of_its_borders(n, k):
+    """Sums of whole numbers below 2^24: exact, whichever kernel takes them."""
+    g = torch.Generator("cuda").manual_seed(n + k)
+    a, b = (torch.randint(-6, 7, (r, k), generator=g, device="cuda").float() for r in (1, n))
+    a[:, ::32], b[:, ::32] = 6, 6
+    qa, qb = lm.mx_quantize(a, "e2m1"), lm.mx_quantize(b, "e2m1")
+    want = qa.dequantize(torch.float32).double() @ qb.dequantize(torch.float32).double().t()
+    assert torch.equal(lm.mx_matmul(qa, qb, torch.float32).double(), want)
+    assert torch.equal(lm.mx_matmul(qb, qa, torch.float32).double(), want.t())
