@@ -143,7 +143,8 @@ def _known(fmt):
 
 
 class DivisionLinear(torch.nn.Linear):
-    """nn.Linear whose products take quantised operands; what it keeps of its input has 8 or 4 bits a number."""
+    """nn.Linear whose products take quantised operands; what it keeps of its input has 8 or 4 bits a number.  For training: the weight is quantised
+    at every call.  To answer with it, lay the weight out once (mx_quantize) and call mx_matmul."""
 
     def __init__(self, in_features, out_features, bias=True, fmt: str = "e4m3", device=None, dtype=None):
         super().__init__(in_features, out_features, bias, device, dtype)
@@ -155,7 +156,8 @@ class DivisionLinear(torch.nn.Linear):
 
 
 class DivisionRMSNorm(torch.nn.Module):
-    """rms_norm with its weight; with a residual it returns (y, h)."""
+    """rms_norm with its weight; with a residual it returns (y, h).  What it keeps of its input has the input's shape and type, and is what
+    `autograd.DivisionCache` compresses, where that takes maps of the kind."""
 
     def __init__(self, features, eps: float = 1e-6, device=None, dtype=None):
         super().__init__()
